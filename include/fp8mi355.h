@@ -61,8 +61,13 @@ enum fp8_flags {
     FP8_OUT_FP32      = 4, /* fp8_scaled_mm writes fp32 instead of bfloat16     */
     FP8_GRAD_WEIGHT_HP = 8, /* recipe flag: dW is computed in bfloat16, not FP8  */
     FP8_EPILOGUE_SIGMOID = 32, /* fp8_scaled_mm: out = bfloat16(sigmoid(result)) instead of bfloat16(result) */
-    FP8_SAVE_FOR_BWD  = 16 /* recipe flag: the forward leaves the transposed fp8 copies of X and W
+    FP8_SAVE_FOR_BWD  = 16, /* recipe flag: the forward leaves the transposed fp8 copies of X and W
                               in the workspace and the backward reuses them                    */
+    FP8_ROUTE_RENORM  = 64, /* fp8_moe_route: gates normalised over the chosen experts          */
+    FP8_ROUTE_FP32    = 128, /* fp8_moe_route: logits (and their gradient) are fp32, not bfloat16 */
+    FP8_ADAMW_PARAM_FP32 = 256, /* fp8_adamw_step: parameters are fp32, not bfloat16            */
+    FP8_ADAMW_GRAD_FP32  = 512, /* fp8_adamw_step: gradients are fp32, not bfloat16             */
+    FP8_ADAMW_STATE_FP8  = 1024 /* fp8_adamw_step: moments as e4m3 codes in blocks, not as fp32  */
 };
 
 enum fp8_status {
@@ -428,6 +433,116 @@ size_t fp8_block_linear_bwd_workspace_bytes(int64_t M, int64_t K, int64_t N);
 int fp8_block_linear_bwd(const void* dy, const void* x, const void* w, int64_t M, int64_t K, int64_t N, int fmt_dy,
                          int fmt_x, int fmt_w, void* dx, void* dw, void* workspace, size_t workspace_bytes,
                          void* stream);
+
+/*
+ * Mixture of experts: the float8 linear layer of E experts, each token going to k
+ * of them.  The calls of a layer, in order:
+ *
+ *   fp8_moe_route             the choice, and the lists below, from the router's logits
+ *   fp8_grouped_linear_fwd    the experts' linear layers over rows ordered by expert
+ *                             (as often as the experts have layers)
+ *   fp8_moe_combine           the gate-weighted sum of each token's rows
+ *   fp8_moe_combine_bwd, fp8_grouped_linear_bwd, fp8_moe_combine (gates NULL: the
+ *   experts' input gradients summed per token), fp8_moe_route_bwd      the way back
+ *
+ * The lists (int32, on the device; the host never learns the group sizes):
+ *   offsets   [E + 1]  expert e has the rows offsets[e] .. offsets[e + 1] - 1; offsets[0] = 0
+ *   row_token [M]      the token behind each row, M = T k; -1 for rows behind the last group
+ *   slot_row  [T, k]   the row of each (token, choice); -1 where there is none
+ * Wrong lists give wrong results and never an access out of bounds: offsets are cut
+ * to a rising sequence within [0, M], tokens and rows out of range count as absent.
+ * Results do not depend on the order in which workgroups run.
+ *
+ * fp8_moe_route: logits [T, E] bfloat16 (fp32 with FP8_ROUTE_FP32), leading dimension
+ *   ld >= E, elements aligned to their size.  The k largest logits of a token, ties to
+ *   the lower expert, in falling order; -inf and NaN are never chosen, so a token may
+ *   get fewer than k experts, or none: those slots have expert -1, gate 0, row -1.
+ *   gates [T, k] fp32 = softmax over all E logits at the chosen ones, or with
+ *   FP8_ROUTE_RENORM over the chosen ones.  experts [T, k].  Rows are ordered by
+ *   (expert, token, choice).  E <= 512, k <= min(E, 16).  workspace:
+ *   fp8_moe_route_workspace_bytes(T, E, k) bytes, 256-byte aligned.
+ * fp8_moe_route_bwd: dlogits [T, E] (type of the logits, ld_out >= E) from dgates
+ *   [T, k] fp32 and the forward's logits, gates and experts:
+ *   p (d - sum_j d_j gate_j), d = dgates at the chosen experts and 0 elsewhere; with
+ *   FP8_ROUTE_RENORM gate (d - sum_j d_j gate_j) at the chosen experts, 0 elsewhere.
+ * fp8_moe_combine: out [T, D] bfloat16 = sum_j gates[t, j] y[slot_row[t, j]], summed
+ *   in fp32 in the order of j; y [M, D] bfloat16; D a multiple of 8; gates NULL: all 1.
+ * fp8_moe_combine_bwd: dy[slot_row[t, j]] = gates[t, j] dout[t] (rows whose row_token is
+ *   not a token are cleared), dgates[t, j] = sum_d dout[t, d] y[slot_row[t, j], d];
+ *   either output may be NULL to skip it.
+ */
+size_t fp8_moe_route_workspace_bytes(int64_t T, int64_t E, int k);
+int fp8_moe_route(const void* logits, int64_t T, int64_t E, int64_t ld, int k, int flags, float* gates,
+                  int32_t* experts, int32_t* offsets, int32_t* row_token, int32_t* slot_row, void* workspace,
+                  size_t workspace_bytes, void* stream);
+int fp8_moe_route_bwd(const float* dgates, const void* logits, int64_t T, int64_t E, int64_t ld, int k, int flags,
+                      const float* gates, const int32_t* experts, void* dlogits, int64_t ld_out, void* stream);
+int fp8_moe_combine(const void* y, int64_t M, int64_t ld, const float* gates, const int32_t* slot_row, int64_t T,
+                    int64_t D, int k, void* out, int64_t ld_out, void* stream);
+int fp8_moe_combine_bwd(const void* dout, int64_t ld_dout, const void* y, int64_t M, int64_t ld, const float* gates,
+                        const int32_t* slot_row, const int32_t* row_token, int64_t T, int64_t D, int k, void* dy,
+                        int64_t ld_dy, float* dgates, void* stream);
+
+/*
+ * the float8 linear layers of E experts over rows grouped by expert (the recipe
+ * FP8_ROW: every operand scaled along the contraction axis of the product it feeds;
+ * flags: FP8_POW2_SCALE only).
+ *   X: the rows x[row_token[r]] of x [T, K] (row_token NULL: x[r], then T = M);
+ *   W [E, N, K]; Y [M, N], dY [M, N], dX [M, K] by row, dW [E, N, K]; bfloat16, dense.
+ * fwd:  Y[r] = X[r] W[e]^T for the rows r of expert e; rows behind the last group are
+ *       written as zeros.  Results are those of fp8_linear_fwd on each group alone, up to the
+ *       order of the sums.
+ * bwd:  dX[r] = dY[r] W[e] (W scaled per column of each expert; rows behind the last
+ *       group: zeros) and dW[e] = dY_e^T X_e (dY and X scaled per column over the rows of
+ *       the group; experts without rows: zeros).  dx or dw may be NULL to skip it.
+ * fwd_prequantized: with weights quantized once, wq [E, N, ldw] codes of format fmt_w and
+ *       scale_w [E, N], as fp8_quantize(w, E N, K, ..., FP8_ROW) makes them.
+ * K % 16 == 0, N % 8 == 0 (backward: 16), M < 2^24; the rows of a group may be any
+ * number, none included.  workspace: what the *_workspace_bytes call returns for the same
+ * arguments, 256-byte aligned.
+ */
+size_t fp8_grouped_linear_workspace_bytes(int64_t M, int64_t E, int64_t K, int64_t N, const fp8_recipe* recipe, int bwd);
+int fp8_grouped_linear_fwd(const void* x, int64_t T, const int32_t* row_token, const void* w, const int32_t* offsets,
+                           int64_t E, int64_t M, int64_t K, int64_t N, const fp8_recipe* recipe, void* y,
+                           void* workspace, size_t workspace_bytes, void* stream);
+int fp8_grouped_linear_bwd(const void* dy, const void* x, int64_t T, const int32_t* row_token, const void* w,
+                           const int32_t* offsets, int64_t E, int64_t M, int64_t K, int64_t N,
+                           const fp8_recipe* recipe, void* dx, void* dw, void* workspace, size_t workspace_bytes,
+                           void* stream);
+size_t fp8_grouped_linear_prequantized_workspace_bytes(int64_t M, int64_t K);
+int fp8_grouped_linear_fwd_prequantized(const void* x, int64_t T, const int32_t* row_token, int fmt_x, int flags,
+                                        const uint8_t* wq, int64_t ldw, int fmt_w, const float* scale_w,
+                                        const int32_t* offsets, int64_t E, int64_t M, int64_t K, int64_t N, void* y,
+                                        void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * AdamW over many tensors, in place:
+ *   g = c grad;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * c = *grad_scale, a number on the device (NULL: 1), e.g. what clipping came to.  All
+ * operations in fp32, each rounded by itself; p rounded once to its own type.
+ * flags: FP8_ADAMW_PARAM_FP32, FP8_ADAMW_GRAD_FP32 (bfloat16 without), the same for
+ * all tensors of a call.  Moments: fp32, or with FP8_ADAMW_STATE_FP8 e4m3 codes in blocks of
+ * 256 consecutive elements (the last of a tensor may be shorter): exp_avg = m * scale_m,
+ * exp_avg_sq = sqrt(v) * scale_v with one power-of-two scale per block, [(n + 255) / 256]
+ * each; a nonzero root is never rounded to zero.  To start, codes of zero with any
+ * power-of-two scales.  This step's update uses the moments before that rounding.
+ * tensors: an array in HOST memory of count descriptors, read before the call returns;
+ * its pointers are device pointers, 16-byte aligned (scales 4).  Up to 60 tensors share a
+ * launch.  step counts from 1; the call holds it, lr and the betas by value, so a captured
+ * graph repeats them.
+ */
+typedef struct fp8_adamw_tensor {
+    void* param;
+    const void* grad;
+    void* exp_avg;
+    void* exp_avg_sq;
+    float* scale_m; /* FP8_ADAMW_STATE_FP8 only */
+    float* scale_v;
+    int64_t n;
+} fp8_adamw_tensor;
+int fp8_adamw_step(const fp8_adamw_tensor* tensors, int64_t count, int flags, double lr, double beta1, double beta2,
+                   double eps, double weight_decay, int64_t step, const float* grad_scale, void* stream);
 
 #ifdef __cplusplus
 }

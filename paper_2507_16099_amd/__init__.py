@@ -5,6 +5,7 @@ streams."""
 from .fp8 import (  # noqa: F401
     FP8_E4M3FN, FP8_E5M2, FP8_TENSOR, FP8_ROW, FP8_COL,
     FP8_POW2_SCALE, FP8_TRANSPOSE_OUT, FP8_OUT_FP32, FP8_GRAD_WEIGHT_HP, FP8_SAVE_FOR_BWD, FP8_EPILOGUE_SIGMOID,
+    FP8_ROUTE_RENORM, FP8_ROUTE_FP32, FP8_ADAMW_PARAM_FP32, FP8_ADAMW_GRAD_FP32, FP8_ADAMW_STATE_FP8, FP8_ADAMW_BLOCK,
     Fp8Error, Recipe, library_path, load_library, set_knob,
     fp8_amax, fp8_scale, fp8_cast, fp8_quantize, fp8_quantize_row_col, fp8_scaled_mm,
     fp8_linear_workspace_bytes, fp8_linear_fwd, fp8_linear_bwd,
@@ -12,5 +13,9 @@ from .fp8 import (  # noqa: F401
     FP8_STATIC_SCRATCH_BYTES, fp8_linear_fwd_prequantized_static,
     fp8_layernorm_quantize, fp8_block_quantize, fp8_block_linear_workspace_bytes, fp8_block_linear_fwd, fp8_block_quantize_t, fp8_block_quantize_row_col, fp8_block_linear_bwd_workspace_bytes, fp8_block_linear_bwd, fp8_linear_bwd_sigmoid_workspace_bytes, fp8_linear_bwd_sigmoid, fp8_mx_quantize, e8m0_plain_rows, fp8_mx_quantize_t, fp8_mx_quantize_row_col, fp8_mx_scaled_mm, fp8_mx_linear_workspace_bytes, fp8_mx_linear_fwd,
     fp8_mx_linear_bwd_workspace_bytes, fp8_mx_linear_bwd,
+    fp8_moe_route_workspace_bytes, fp8_moe_route, fp8_moe_route_bwd, fp8_moe_combine, fp8_moe_combine_bwd,
+    fp8_grouped_linear_workspace_bytes, fp8_grouped_linear_fwd, fp8_grouped_linear_bwd,
+    fp8_grouped_linear_prequantized_workspace_bytes, fp8_grouped_linear_fwd_prequantized,
+    AdamwTensors, fp8_adamw_tensors, fp8_adamw_step,
     fp8_last_error, fp8_version,
 )

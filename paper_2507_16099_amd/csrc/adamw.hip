@@ -1,0 +1,250 @@
+// One AdamW step over many tensors:
+//   g' = c g;  m = b1 m + (1 - b1) g';  v = b2 v + (1 - b2) g'^2
+//   p = p (1 - lr wd) - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
+// in binary32, one rounding per operation in this order; p and g in bfloat16 or binary32 (c: a number on the device, what clipping
+// has come to).
+//
+// Moments in 32 bits, or in 8: e4m3 codes in blocks of 256 elements with one power-of-two scale each, so that the only rounding
+// is the code's.  Of the second moment the square root is kept: e4m3 spans 2^-9 .. 448, which for the root is 2^36 between the
+// largest and the smallest v of a block, and a root's half step of 6 % is 3 % on each side of what divides the update.  A root that is not
+// zero is never stored as zero (it would leave m / eps): it becomes the smallest code.  The update of this step uses m and v from before
+// the rounding.
+//
+// The tensors of a launch lie in its arguments (up to 64 of them, no table in memory); a workgroup takes a piece of one of them.
+// Bound: HBM, 10 bytes an element (bfloat16, 8-bit moments) to 28 (all binary32).
+#include "fp8_device.hpp"
+#include "moe_launchers.hpp"
+
+namespace fp8k {
+
+namespace {
+
+constexpr int NT = 256;
+constexpr int PIECE = 8192;       // elements of a workgroup
+constexpr int MOST = 60;          // tensors of a launch: the arguments hold 4 KB
+
+struct Many {
+    AdamwTensor t[MOST];
+    int first[MOST + 1];          // its first workgroup
+    int count;
+};
+static_assert(sizeof(Many) + sizeof(AdamwScalars) <= 4096, "kernel arguments");
+
+struct Update {
+    AdamwScalars s;
+    float c;
+    __device__ __forceinline__ void moments(float g, float& m, float& v) const {
+        g = __fmul_rn(g, c);
+        m = __fadd_rn(__fmul_rn(m, s.b1), __fmul_rn(g, s.c1));
+        v = __fadd_rn(__fmul_rn(v, s.b2), __fmul_rn(__fmul_rn(g, g), s.c2));
+    }
+    __device__ __forceinline__ float param(float p, float m, float root) const {
+        const float d = __fadd_rn(__fmul_rn(root, s.inv_root), s.eps);
+        return __fsub_rn(__fmul_rn(p, s.decay), __fmul_rn(__fdiv_rn(m, d), s.rate));
+    }
+};
+
+__device__ __forceinline__ float get(const float* p, int64_t i) { return p[i]; }
+__device__ __forceinline__ float get(const __bf16* p, int64_t i) { return (float)p[i]; }
+
+// eight elements at p; those from n on are zero
+template <class T>
+__device__ __forceinline__ void load8(const T* p, int n, float (&f)[8]) {
+    if (n >= 8) {
+        if constexpr (sizeof(T) == 2) {
+            const uint4 v = load_stream(p);
+            f[0] = bf16_lo(v.x); f[1] = bf16_hi(v.x); f[2] = bf16_lo(v.y); f[3] = bf16_hi(v.y);
+            f[4] = bf16_lo(v.z); f[5] = bf16_hi(v.z); f[6] = bf16_lo(v.w); f[7] = bf16_hi(v.w);
+        } else {
+            const uint4 a = load_stream(p), b = load_stream(p + 4);
+            f[0] = __uint_as_float(a.x); f[1] = __uint_as_float(a.y); f[2] = __uint_as_float(a.z); f[3] = __uint_as_float(a.w);
+            f[4] = __uint_as_float(b.x); f[5] = __uint_as_float(b.y); f[6] = __uint_as_float(b.z); f[7] = __uint_as_float(b.w);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = i < n ? get(p, i) : 0.f;
+    }
+}
+typedef __bf16 bf16x2_a __attribute__((ext_vector_type(2)));
+typedef float f32x2_a __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    const f32x2_a v = {a, b};
+    const bf16x2_a h = __builtin_convertvector(v, bf16x2_a);
+    uint32_t r;
+    __builtin_memcpy(&r, &h, 4);
+    return r;
+}
+template <class T>
+__device__ __forceinline__ void store8(T* p, int n, const float (&f)[8]) {
+    if (n >= 8) {
+        if constexpr (sizeof(T) == 2) {
+            store_nt(p, make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7])));
+        } else {
+            store_nt(p, make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])));
+            store_nt(p + 4, make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = (T)f[i];
+    }
+}
+// eight codes at q as values
+__device__ __forceinline__ void load_codes(const uint8_t* q, int n, float (&f)[8]) {
+    uint2 c = make_uint2(0, 0);
+    if (n >= 8) {
+        c = *reinterpret_cast<const uint2*>(q);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) (i < 4 ? c.x : c.y) |= (uint32_t)q[i] << (8 * (i & 3));
+    }
+    f[0] = __builtin_amdgcn_cvt_f32_fp8((int)c.x, 0); f[1] = __builtin_amdgcn_cvt_f32_fp8((int)c.x, 1);
+    f[2] = __builtin_amdgcn_cvt_f32_fp8((int)c.x, 2); f[3] = __builtin_amdgcn_cvt_f32_fp8((int)c.x, 3);
+    f[4] = __builtin_amdgcn_cvt_f32_fp8((int)c.y, 0); f[5] = __builtin_amdgcn_cvt_f32_fp8((int)c.y, 1);
+    f[6] = __builtin_amdgcn_cvt_f32_fp8((int)c.y, 2); f[7] = __builtin_amdgcn_cvt_f32_fp8((int)c.y, 3);
+}
+__device__ __forceinline__ void store_codes(uint8_t* q, int n, const float (&f)[8]) {
+    const uint2 c = make_uint2(cvt4<FMT_E4M3FN>(f[0], f[1], f[2], f[3]), cvt4<FMT_E4M3FN>(f[4], f[5], f[6], f[7]));
+    if (n >= 8) {
+        *reinterpret_cast<uint2*>(q) = c;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) q[i] = (uint8_t)((i < 4 ? c.x : c.y) >> (8 * (i & 3)));
+    }
+}
+// largest magnitude of the 32 lanes' eight values each; all 32 get it
+__device__ __forceinline__ float block_amax(const float (&f)[8]) {
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(f[i]));
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+    return m;
+}
+
+// scale_from_amax(amax, FMT_E4M3FN, FLAG_POW2) from the exponent: 448 = 1.75 2^8, so 2^(8 - e) where the significand is at most 1.75,
+// else half of that, and 2^48 at most (the clamp of amax at 1e-12).  The binary64 division there is as much work as all else here.
+__device__ __forceinline__ float state_scale(float amax) {
+    const int b = (int)(__float_as_uint(amax) & 0x7FFFFFFFu);
+    const int e = 262 - (b >> 23) - ((b & 0x7FFFFF) > 0x600000 ? 1 : 0);
+    return __uint_as_float((uint32_t)(e < 175 ? e : 175) << 23);
+}
+// 1 / s of a power of two; of zero (a state that was never written) something finite
+__device__ __forceinline__ float inverse_pow2(float s) { return __uint_as_float((254u - (__float_as_uint(s) >> 23 & 0xFFu)) << 23); }
+
+// a thread: eight elements at a time; 32 lanes hold a block of 256
+template <class P, class G, bool FP8>
+__global__ __launch_bounds__(NT) void adamw_kernel(Many many, AdamwScalars s) {
+    int lo = 0, hi = many.count;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (many.first[mid] <= (int)blockIdx.x) lo = mid;
+        else hi = mid;
+    }
+    const AdamwTensor t = many.t[lo];
+    const int64_t i0 = (int64_t)((int)blockIdx.x - many.first[lo]) * PIECE;
+    const Update u{s, s.grad_scale ? *s.grad_scale : 1.0f};
+    P* p = static_cast<P*>(t.p);
+    const G* g = static_cast<const G*>(t.g);
+#pragma unroll 2
+    for (int r = 0; r < PIECE / (NT * 8); ++r) {
+        const int64_t i = i0 + (int64_t)(r * NT + (int)threadIdx.x) * 8;
+        const int64_t left = t.n - i;
+        const int n = left >= 8 ? 8 : left > 0 ? (int)left : 0;
+        if (!FP8 && n == 0) return;
+        float fp[8], fg[8], m[8], v[8], root[8];
+        load8(p + i, n, fp);
+        load8(g + i, n, fg);
+        if constexpr (FP8) {
+            const float inv_m = n ? inverse_pow2(t.sm[i / 256]) : 0.f, inv_v = n ? inverse_pow2(t.sv[i / 256]) : 0.f;
+            load_codes(static_cast<const uint8_t*>(t.m) + i, n, m);
+            load_codes(static_cast<const uint8_t*>(t.v) + i, n, root);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                m[e] *= inv_m;
+                const float ro = root[e] * inv_v;
+                v[e] = __fmul_rn(ro, ro);
+            }
+        } else {
+            load8(static_cast<const float*>(t.m) + i, n, m);
+            load8(static_cast<const float*>(t.v) + i, n, v);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            u.moments(fg[e], m[e], v[e]);
+            root[e] = __fsqrt_rn(v[e]);
+            fp[e] = u.param(fp[e], m[e], root[e]);
+        }
+        store8(p + i, n, fp);
+        if constexpr (FP8) {
+            const float sm = state_scale(block_amax(m)), sv = state_scale(block_amax(root));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                m[e] *= sm;
+                root[e] = root[e] > 0.f ? fmaxf(root[e] * sv, 0x1p-9f) : root[e];
+            }
+            store_codes(static_cast<uint8_t*>(t.m) + i, n, m);
+            store_codes(static_cast<uint8_t*>(t.v) + i, n, root);
+            if (n && threadIdx.x % 32 == 0) {
+                t.sm[i / 256] = sm;
+                t.sv[i / 256] = sv;
+            }
+        } else {
+            store8(static_cast<float*>(t.m) + i, n, m);
+            store8(static_cast<float*>(t.v) + i, n, v);
+        }
+    }
+}
+
+template <class P, class G>
+hipError_t launch_t(const Many& many, const AdamwScalars& s, bool fp8_state, hipStream_t st) {
+    const unsigned grid = (unsigned)many.first[many.count];
+    if (fp8_state) adamw_kernel<P, G, true><<<grid, NT, 0, st>>>(many, s);
+    else adamw_kernel<P, G, false><<<grid, NT, 0, st>>>(many, s);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_adamw(const AdamwTensor* tensors, int64_t count, bool p_f32, bool g_f32, bool fp8_state, const AdamwScalars& s, hipStream_t st) {
+    Many many;
+    many.count = 0;
+    many.first[0] = 0;
+    auto flush = [&]() -> hipError_t {
+        if (many.count == 0) return hipSuccess;
+        const hipError_t e = p_f32 ? (g_f32 ? launch_t<float, float>(many, s, fp8_state, st) : launch_t<float, __bf16>(many, s, fp8_state, st))
+                                   : (g_f32 ? launch_t<__bf16, float>(many, s, fp8_state, st) : launch_t<__bf16, __bf16>(many, s, fp8_state, st));
+        many.count = 0;
+        return e;
+    };
+    for (int64_t i = 0; i < count; ++i) {
+        AdamwTensor t = tensors[i];
+        while (t.n > 0) {
+            const int64_t room = (1 << 23) - (int64_t)(many.count ? many.first[many.count] : 0);      // workgroups left in the launch (a grid's threads are counted in 32 bits)
+            const int64_t want = (t.n + PIECE - 1) / PIECE, take = want < room ? want : room;
+            AdamwTensor part = t;
+            if (take < want) part.n = take * PIECE;
+            many.t[many.count] = part;
+            many.first[many.count + 1] = many.first[many.count] + (int)take;
+            ++many.count;
+            if (many.count == MOST || take < want)
+                if (hipError_t e = flush(); e != hipSuccess) return e;
+            if (take < want) {
+                const int64_t d = take * PIECE;
+                t.p = static_cast<char*>(t.p) + d * (p_f32 ? 4 : 2);
+                t.g = static_cast<const char*>(t.g) + d * (g_f32 ? 4 : 2);
+                t.m = static_cast<char*>(t.m) + d * (fp8_state ? 1 : 4);
+                t.v = static_cast<char*>(t.v) + d * (fp8_state ? 1 : 4);
+                if (fp8_state) { t.sm += d / 256; t.sv += d / 256; }
+                t.n -= d;
+            } else {
+                t.n = 0;
+            }
+        }
+    }
+    return flush();
+}
+
+}  // namespace fp8k

@@ -3,6 +3,7 @@
 // Every entry point validates on the host, then only enqueues work.
 #include "../../include/fp8mi355.h"
 #include "launchers.hpp"
+#include "moe_launchers.hpp"
 
 #include <atomic>
 #include <cstdarg>
@@ -244,6 +245,11 @@ int check_linear_dims(const char* fn, int64_t M, int64_t K, int64_t N, bool bwd)
 }
 
 }  // namespace
+
+// for the entry points of the other files: the text of an error ("" clears it)
+namespace fp8k {
+int api_error(int code, const char* text) { return fail(code, "%s", text); }
+}  // namespace fp8k
 
 extern "C" {
 

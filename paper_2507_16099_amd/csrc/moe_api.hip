@@ -1,0 +1,370 @@
+// C ABI of the mixture-of-experts operators and of the AdamW step: argument validation, workspace planning and the composition out
+// of the kernels.  Every entry point validates on the host, then only enqueues work.
+#include "../../include/fp8mi355.h"
+#include "launchers.hpp"
+#include "moe_launchers.hpp"
+
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+
+namespace {
+
+using fp8k::api_error;
+
+int fail(int code, const char* fmt, ...) {
+    char text[256];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(text, sizeof(text), fmt, ap);
+    va_end(ap);
+    return api_error(code, text);
+}
+
+#define FP8_TRY(expr)                                                                                              \
+    do {                                                                                                           \
+        hipError_t e__ = (expr);                                                                                   \
+        if (e__ != hipSuccess) return fail(FP8_ERR_HIP, "%s: %s", #expr, hipGetErrorString(e__));                  \
+    } while (0)
+#define FP8_CHECK(expr)                   \
+    do {                                  \
+        if (int rc__ = (expr)) return rc__; \
+    } while (0)
+
+typedef long long ll;
+
+bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+bool fmt_ok(int f) { return f == FP8_E4M3FN || f == FP8_E5M2; }
+constexpr int64_t kMaxDim = 0x7FFFFFFF;
+// rows: a grid of one workgroup each counts its threads in 32 bits; leading dimensions: the products' offsets inside a tile are 32 bits
+constexpr int64_t kMaxRows = (1 << 24) - 1, kMaxLd = (1 << 23) - 1;
+
+size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+
+int need(const char* fn, const char* what, const void* p, size_t align) {
+    if (!p) return fail(FP8_ERR_NULL, "%s: %s is NULL", fn, what);
+    if (!aligned(p, align)) return fail(FP8_ERR_ALIGN, "%s: %s not %zu-byte aligned", fn, what, align);
+    return FP8_OK;
+}
+int need_ld(const char* fn, const char* what, int64_t ld, int64_t cols, int64_t unit) {
+    if (ld < cols) return fail(FP8_ERR_SHAPE, "%s: ld of %s = %lld < %lld", fn, what, (ll)ld, (ll)cols);
+    if (ld % unit) return fail(FP8_ERR_ALIGN, "%s: ld of %s = %lld not a multiple of %lld", fn, what, (ll)ld, (ll)unit);
+    return FP8_OK;
+}
+
+// ---- router ----------------------------------------------------------------------------------------------------------
+
+int check_route(const char* fn, int64_t T, int64_t E, int64_t ld, int k, int flags) {
+    if (flags & ~(FP8_ROUTE_RENORM | FP8_ROUTE_FP32)) return fail(FP8_ERR_ENUM, "%s: flags=%d has unknown bits", fn, flags);
+    if (T < 0 || T > kMaxDim) return fail(FP8_ERR_SHAPE, "%s: T=%lld out of range", fn, (ll)T);
+    if (E < 1 || E > fp8k::ROUTE_MAX_EXPERTS) return fail(FP8_ERR_SHAPE, "%s: E=%lld, 1 .. %d are supported", fn, (ll)E, fp8k::ROUTE_MAX_EXPERTS);
+    if (k < 1 || k > fp8k::ROUTE_MAX_K || k > E) return fail(FP8_ERR_SHAPE, "%s: k=%d, 1 .. min(E, %d) are supported", fn, k, fp8k::ROUTE_MAX_K);
+    if (T * k > kMaxDim) return fail(FP8_ERR_SHAPE, "%s: T k = %lld out of range", fn, (ll)(T * k));
+    if (ld < E) return fail(FP8_ERR_SHAPE, "%s: ld=%lld < E=%lld", fn, (ll)ld, (ll)E);
+    return FP8_OK;
+}
+
+// ---- grouped linear --------------------------------------------------------------------------------------------------
+
+// leading dimension of codes that are contracted over n elements: whole cache lines once a row is longer than four
+int64_t pitch(int64_t n) { return n <= 512 ? (n + 15) / 16 * 16 : (n + 127) / 128 * 128; }
+
+struct FwdPlan { size_t xq, wq, sx, sw, total; };
+struct BwdPlan { size_t gq, sg, wt, swt, gt, sgt, xt, sxt, amax, total; };
+
+FwdPlan plan_fwd(int64_t M, int64_t E, int64_t K, int64_t N, bool with_w) {
+    FwdPlan p{};
+    size_t o = 0;
+    auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes, 256); return at; };
+    p.xq = take((size_t)M * pitch(K));
+    p.sx = take((size_t)M * 4);
+    p.wq = take(with_w ? (size_t)E * N * pitch(K) : 0);
+    p.sw = take(with_w ? (size_t)E * N * 4 : 0);
+    p.total = o;
+    return p;
+}
+BwdPlan plan_bwd(int64_t M, int64_t E, int64_t K, int64_t N) {
+    BwdPlan p{};
+    size_t o = 0;
+    auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes, 256); return at; };
+    const size_t Mp = (size_t)fp8k::grouped_padded(M, E);
+    p.gq = take((size_t)M * pitch(N));           // dY codes [M, N]
+    p.sg = take((size_t)M * 4);
+    p.wt = take((size_t)E * K * pitch(N));       // W codes [E, K, N], scales [E, K]
+    p.swt = take((size_t)E * K * 4);
+    p.gt = take((size_t)N * Mp);                 // dY codes [N, padded rows], scales [E, N]
+    p.sgt = take((size_t)E * N * 4);
+    p.xt = take((size_t)K * Mp);                 // X codes [K, padded rows], scales [E, K]
+    p.sxt = take((size_t)E * K * 4);
+    p.amax = take((size_t)E * (K > N ? K : N) * 4);
+    p.total = o;
+    return p;
+}
+
+int check_dims(const char* fn, int64_t T, int64_t M, int64_t E, int64_t K, int64_t N, bool bwd) {
+    if (T < 0 || T > kMaxDim || M < 0 || M > kMaxRows || E < 1 || E > kMaxRows || K < 0 || N < 0)
+        return fail(FP8_ERR_SHAPE, "%s: T=%lld M=%lld E=%lld K=%lld N=%lld out of range", fn, (ll)T, (ll)M, (ll)E, (ll)K, (ll)N);
+    if (K > kMaxLd - 127 || N > kMaxLd - 127 || E * K > kMaxDim || E * N > kMaxDim)
+        return fail(FP8_ERR_SHAPE, "%s: E=%lld K=%lld N=%lld out of range", fn, (ll)E, (ll)K, (ll)N);
+    if (K % 16) return fail(FP8_ERR_SHAPE, "%s: K=%lld must be a multiple of 16", fn, (ll)K);
+    if (N % 8) return fail(FP8_ERR_SHAPE, "%s: N=%lld must be a multiple of 8 (dense bfloat16 rows)", fn, (ll)N);
+    if (bwd && N % 16) return fail(FP8_ERR_SHAPE, "%s: the backward contracts over N: N=%lld must be a multiple of 16", fn, (ll)N);
+    if (bwd && fp8k::grouped_padded(M, E) > kMaxLd)
+        return fail(FP8_ERR_SHAPE, "%s: M=%lld rows in E=%lld groups, each padded to 128, are out of range", fn, (ll)M, (ll)E);
+    return FP8_OK;
+}
+int check_recipe(const char* fn, const fp8_recipe* r) {
+    if (!r) return fail(FP8_ERR_NULL, "%s: recipe is NULL", fn);
+    if (r->gran != FP8_ROW) return fail(FP8_ERR_ENUM, "%s: recipe.gran=%d must be FP8_ROW", fn, r->gran);
+    if (!fmt_ok(r->fmt_x) || !fmt_ok(r->fmt_w) || !fmt_ok(r->fmt_dy)) return fail(FP8_ERR_ENUM, "%s: unknown fp8 format in recipe", fn);
+    if (r->flags & ~FP8_POW2_SCALE) return fail(FP8_ERR_ENUM, "%s: recipe.flags=%d has bits that grouped products do not take", fn, r->flags);
+    return FP8_OK;
+}
+int check_rows(const char* fn, const int32_t* row_token, int64_t T, int64_t M) {
+    if (!aligned(row_token, 4)) return fail(FP8_ERR_ALIGN, "%s: row_token not 4-byte aligned", fn);
+    if (!row_token && T != M) return fail(FP8_ERR_SHAPE, "%s: without row_token x has a row per row: T=%lld, M=%lld", fn, (ll)T, (ll)M);
+    return FP8_OK;
+}
+int check_workspace(const char* fn, const void* ws, size_t have, size_t want) {
+    FP8_CHECK(need(fn, "workspace", ws, 256));
+    if (have < want) return fail(FP8_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", fn, have, want);
+    return FP8_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t fp8_moe_route_workspace_bytes(int64_t T, int64_t E, int k) {
+    api_error(FP8_OK, "");
+    if (check_route("fp8_moe_route_workspace_bytes", T, E, E, k, 0)) return 0;
+    return fp8k::route_workspace_bytes(T, E);
+}
+
+int fp8_moe_route(const void* logits, int64_t T, int64_t E, int64_t ld, int k, int flags, float* gates, int32_t* experts, int32_t* offsets,
+                  int32_t* row_token, int32_t* slot_row, void* workspace, size_t workspace_bytes, void* stream) {
+    const char* fn = "fp8_moe_route";
+    api_error(FP8_OK, "");
+    FP8_CHECK(check_route(fn, T, E, ld, k, flags));
+    FP8_CHECK(need(fn, "offsets", offsets, 4));
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (T == 0) {      // (an empty batch has its E + 1 zeros all the same)
+        FP8_TRY(fp8k::launch_fill_u32(reinterpret_cast<uint32_t*>(offsets), E + 1, 0u, st));
+        return FP8_OK;
+    }
+    const bool f32 = flags & FP8_ROUTE_FP32;
+    FP8_CHECK(need(fn, "logits", logits, f32 ? 4 : 2));
+    FP8_CHECK(need(fn, "gates", gates, 4));
+    FP8_CHECK(need(fn, "experts", experts, 4));
+    FP8_CHECK(need(fn, "row_token", row_token, 4));
+    FP8_CHECK(need(fn, "slot_row", slot_row, 4));
+    FP8_CHECK(check_workspace(fn, workspace, workspace_bytes, fp8k::route_workspace_bytes(T, E)));
+    FP8_TRY(fp8k::launch_moe_route(logits, f32, T, E, ld, k, flags & FP8_ROUTE_RENORM, gates, experts, offsets, row_token, slot_row, workspace, st));
+    return FP8_OK;
+}
+
+int fp8_moe_route_bwd(const float* dgates, const void* logits, int64_t T, int64_t E, int64_t ld, int k, int flags, const float* gates,
+                      const int32_t* experts, void* dlogits, int64_t ld_out, void* stream) {
+    const char* fn = "fp8_moe_route_bwd";
+    api_error(FP8_OK, "");
+    FP8_CHECK(check_route(fn, T, E, ld, k, flags));
+    if (ld_out < E) return fail(FP8_ERR_SHAPE, "%s: ld_out=%lld < E=%lld", fn, (ll)ld_out, (ll)E);
+    if (T == 0) return FP8_OK;
+    const bool f32 = flags & FP8_ROUTE_FP32;
+    FP8_CHECK(need(fn, "dgates", dgates, 4));
+    FP8_CHECK(need(fn, "logits", logits, f32 ? 4 : 2));
+    FP8_CHECK(need(fn, "gates", gates, 4));
+    FP8_CHECK(need(fn, "experts", experts, 4));
+    FP8_CHECK(need(fn, "dlogits", dlogits, f32 ? 4 : 2));
+    FP8_TRY(fp8k::launch_moe_route_bwd(dgates, logits, f32, T, E, ld, k, flags & FP8_ROUTE_RENORM, gates, experts, dlogits, ld_out,
+                                       static_cast<hipStream_t>(stream)));
+    return FP8_OK;
+}
+
+static int check_combine(const char* fn, int64_t M, int64_t T, int64_t D, int k) {
+    if (M < 0 || M > kMaxDim || T < 0 || T > kMaxDim || D < 0 || D > kMaxDim || k < 1 || T * k > kMaxDim)
+        return fail(FP8_ERR_SHAPE, "%s: M=%lld T=%lld D=%lld k=%d out of range", fn, (ll)M, (ll)T, (ll)D, k);
+    if (D % 8) return fail(FP8_ERR_SHAPE, "%s: D=%lld must be a multiple of 8", fn, (ll)D);
+    if (T * (D / 8) > (int64_t)1 << 31) return fail(FP8_ERR_SHAPE, "%s: T D = %lld out of range", fn, (ll)(T * D));
+    return FP8_OK;
+}
+
+int fp8_moe_combine(const void* y, int64_t M, int64_t ld, const float* gates, const int32_t* slot_row, int64_t T, int64_t D, int k, void* out,
+                    int64_t ld_out, void* stream) {
+    const char* fn = "fp8_moe_combine";
+    api_error(FP8_OK, "");
+    FP8_CHECK(check_combine(fn, M, T, D, k));
+    FP8_CHECK(need_ld(fn, "y", ld, D, 8));
+    FP8_CHECK(need_ld(fn, "out", ld_out, D, 8));
+    if (T == 0 || D == 0) return FP8_OK;
+    if (M > 0) FP8_CHECK(need(fn, "y", y, 16));
+    FP8_CHECK(need(fn, "slot_row", slot_row, 4));
+    FP8_CHECK(need(fn, "out", out, 16));
+    if (!aligned(gates, 4)) return fail(FP8_ERR_ALIGN, "%s: gates not 4-byte aligned", fn);
+    FP8_TRY(fp8k::launch_moe_combine(y, M, ld, gates, slot_row, T, D, k, out, ld_out, static_cast<hipStream_t>(stream)));
+    return FP8_OK;
+}
+
+int fp8_moe_combine_bwd(const void* dout, int64_t ld_dout, const void* y, int64_t M, int64_t ld, const float* gates, const int32_t* slot_row,
+                        const int32_t* row_token, int64_t T, int64_t D, int k, void* dy, int64_t ld_dy, float* dgates, void* stream) {
+    const char* fn = "fp8_moe_combine_bwd";
+    api_error(FP8_OK, "");
+    FP8_CHECK(check_combine(fn, M, T, D, k));
+    FP8_CHECK(need_ld(fn, "dout", ld_dout, D, 8));
+    if (dgates) FP8_CHECK(need_ld(fn, "y", ld, D, 8));
+    if (dy) FP8_CHECK(need_ld(fn, "dy", ld_dy, D, 8));
+    if (!dy && !dgates) return FP8_OK;
+    if (T + (M + 63) / 64 > kMaxRows) return fail(FP8_ERR_SHAPE, "%s: T=%lld M=%lld out of range", fn, (ll)T, (ll)M);
+    if (T == 0 && M == 0) return FP8_OK;
+    if (T > 0 && D > 0) FP8_CHECK(need(fn, "dout", dout, 16));
+    if (T > 0) FP8_CHECK(need(fn, "slot_row", slot_row, 4));
+    if (dgates && M > 0 && D > 0) FP8_CHECK(need(fn, "y", y, 16));
+    if (dy && M > 0) FP8_CHECK(need(fn, "row_token", row_token, 4));
+    if (!aligned(dy, 16)) return fail(FP8_ERR_ALIGN, "%s: dy not 16-byte aligned", fn);
+    if (!aligned(gates, 4) || !aligned(dgates, 4)) return fail(FP8_ERR_ALIGN, "%s: gates not 4-byte aligned", fn);
+    FP8_TRY(fp8k::launch_moe_combine_bwd(dout, ld_dout, y, ld, gates, slot_row, row_token, M, T, D, k, dy, ld_dy, dgates,
+                                         static_cast<hipStream_t>(stream)));
+    return FP8_OK;
+}
+
+size_t fp8_grouped_linear_workspace_bytes(int64_t M, int64_t E, int64_t K, int64_t N, const fp8_recipe* recipe, int bwd) {
+    const char* fn = "fp8_grouped_linear_workspace_bytes";
+    api_error(FP8_OK, "");
+    if (check_recipe(fn, recipe) || check_dims(fn, 0, M, E, K, N, bwd)) return 0;
+    const size_t n = bwd ? plan_bwd(M, E, K, N).total : plan_fwd(M, E, K, N, true).total;
+    return n ? n : 256;
+}
+
+int fp8_grouped_linear_fwd(const void* x, int64_t T, const int32_t* row_token, const void* w, const int32_t* offsets, int64_t E, int64_t M,
+                           int64_t K, int64_t N, const fp8_recipe* recipe, void* y, void* workspace, size_t workspace_bytes, void* stream) {
+    const char* fn = "fp8_grouped_linear_fwd";
+    api_error(FP8_OK, "");
+    FP8_CHECK(check_recipe(fn, recipe));
+    FP8_CHECK(check_dims(fn, T, M, E, K, N, false));
+    FP8_CHECK(check_rows(fn, row_token, T, M));
+    if (M == 0 || N == 0 || K == 0) return FP8_OK;
+    FP8_CHECK(need(fn, "offsets", offsets, 4));
+    FP8_CHECK(need(fn, "y", y, 16));
+    FP8_CHECK(need(fn, "w", w, 16));
+    if (T > 0) FP8_CHECK(need(fn, "x", x, 16));
+    const FwdPlan p = plan_fwd(M, E, K, N, true);
+    FP8_CHECK(check_workspace(fn, workspace, workspace_bytes, p.total));
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    float *sx = reinterpret_cast<float*>(ws + p.sx), *sw = reinterpret_cast<float*>(ws + p.sw);
+    const int64_t ld = pitch(K);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int fl = recipe->flags & FP8_POW2_SCALE;
+    FP8_TRY(fp8k::launch_quant_rows_gather(x, T, K, row_token, M, K, recipe->fmt_x, fl, ws + p.xq, ld, sx, st));
+    FP8_CHECK(fp8_quantize(w, E * N, K, K, FP8_ROW, recipe->fmt_w, fl, ws + p.wq, ld, sw, stream));
+    FP8_TRY(fp8k::launch_gemm_fp8_grouped_rows({ws + p.xq, ld, recipe->fmt_x, sx, ws + p.wq, ld, recipe->fmt_w, sw, offsets, E, M, N, K, y, N}, st));
+    return FP8_OK;
+}
+
+int fp8_grouped_linear_bwd(const void* dy, const void* x, int64_t T, const int32_t* row_token, const void* w, const int32_t* offsets, int64_t E,
+                           int64_t M, int64_t K, int64_t N, const fp8_recipe* recipe, void* dx, void* dw, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+    const char* fn = "fp8_grouped_linear_bwd";
+    api_error(FP8_OK, "");
+    FP8_CHECK(check_recipe(fn, recipe));
+    FP8_CHECK(check_dims(fn, T, M, E, K, N, true));
+    FP8_CHECK(check_rows(fn, row_token, T, M));
+    if (K == 0 || N == 0 || (!dx && !dw)) return FP8_OK;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (!aligned(dx, 16) || !aligned(dw, 16)) return fail(FP8_ERR_ALIGN, "%s: dx, dw not 16-byte aligned", fn);
+    if (M == 0) {      // no rows: the weights' gradients are zero
+        if (dw) FP8_TRY(fp8k::launch_fill_u32(static_cast<uint32_t*>(dw), E * N * K / 2, 0u, st));
+        return FP8_OK;
+    }
+    FP8_CHECK(need(fn, "offsets", offsets, 4));
+    FP8_CHECK(need(fn, "dy", dy, 16));
+    if (dx) FP8_CHECK(need(fn, "w", w, 16));
+    if (dw && T > 0) FP8_CHECK(need(fn, "x", x, 16));
+    const BwdPlan p = plan_bwd(M, E, K, N);
+    FP8_CHECK(check_workspace(fn, workspace, workspace_bytes, p.total));
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    auto f32 = [&](size_t at) { return reinterpret_cast<float*>(ws + at); };
+    uint32_t* amax = reinterpret_cast<uint32_t*>(ws + p.amax);
+    const int64_t ld = pitch(N), Mp = fp8k::grouped_padded(M, E);
+    const int fl = recipe->flags & FP8_POW2_SCALE;
+    if (dx) {
+        FP8_TRY(fp8k::launch_quant_rows_gather(dy, M, N, nullptr, M, N, recipe->fmt_dy, fl, ws + p.gq, ld, f32(p.sg), st));
+        FP8_TRY(fp8k::launch_quant_cols_grouped({w, E * N, K, nullptr, E * N, K, recipe->fmt_w, ws + p.wt, ld, f32(p.swt), amax}, nullptr, E, fl, st));
+        FP8_TRY(fp8k::launch_gemm_fp8_grouped_rows({ws + p.gq, ld, recipe->fmt_dy, f32(p.sg), ws + p.wt, ld, recipe->fmt_w, f32(p.swt), offsets, E, M,
+                                                    K, N, dx, K}, st));
+    }
+    if (dw) {
+        FP8_TRY(fp8k::launch_quant_cols_grouped({dy, M, N, nullptr, M, N, recipe->fmt_dy, ws + p.gt, Mp, f32(p.sgt), amax}, offsets, E, fl, st));
+        FP8_TRY(fp8k::launch_quant_cols_grouped({x, T, K, row_token, M, K, recipe->fmt_x, ws + p.xt, Mp, f32(p.sxt), amax}, offsets, E, fl, st));
+        FP8_TRY(fp8k::launch_gemm_fp8_grouped_contract({ws + p.gt, Mp, recipe->fmt_dy, f32(p.sgt), ws + p.xt, Mp, recipe->fmt_x, f32(p.sxt), offsets,
+                                                        E, M, N, K, dw, K}, st));
+    }
+    return FP8_OK;
+}
+
+size_t fp8_grouped_linear_prequantized_workspace_bytes(int64_t M, int64_t K) {
+    const char* fn = "fp8_grouped_linear_prequantized_workspace_bytes";
+    api_error(FP8_OK, "");
+    if (check_dims(fn, 0, M, 1, K, 0, false)) return 0;
+    const size_t n = plan_fwd(M, 1, K, 0, false).total;
+    return n ? n : 256;
+}
+
+int fp8_grouped_linear_fwd_prequantized(const void* x, int64_t T, const int32_t* row_token, int fmt_x, int flags, const uint8_t* wq, int64_t ldw,
+                                        int fmt_w, const float* scale_w, const int32_t* offsets, int64_t E, int64_t M, int64_t K, int64_t N,
+                                        void* y, void* workspace, size_t workspace_bytes, void* stream) {
+    const char* fn = "fp8_grouped_linear_fwd_prequantized";
+    api_error(FP8_OK, "");
+    if (!fmt_ok(fmt_x) || !fmt_ok(fmt_w)) return fail(FP8_ERR_ENUM, "%s: unknown fp8 format", fn);
+    if (flags & ~FP8_POW2_SCALE) return fail(FP8_ERR_ENUM, "%s: flags=%d has unknown bits", fn, flags);
+    FP8_CHECK(check_dims(fn, T, M, E, K, N, false));
+    FP8_CHECK(check_rows(fn, row_token, T, M));
+    FP8_CHECK(need_ld(fn, "wq", ldw, K, 16));
+    if (ldw > kMaxLd) return fail(FP8_ERR_SHAPE, "%s: ldw=%lld out of range", fn, (ll)ldw);
+    if (M == 0 || N == 0 || K == 0) return FP8_OK;
+    FP8_CHECK(need(fn, "offsets", offsets, 4));
+    FP8_CHECK(need(fn, "y", y, 16));
+    FP8_CHECK(need(fn, "scale_w", scale_w, 4));
+    FP8_CHECK(need(fn, "wq", wq, 16));
+    if (T > 0) FP8_CHECK(need(fn, "x", x, 16));
+    const FwdPlan p = plan_fwd(M, 1, K, 0, false);
+    FP8_CHECK(check_workspace(fn, workspace, workspace_bytes, p.total));
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    float* sx = reinterpret_cast<float*>(ws + p.sx);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    FP8_TRY(fp8k::launch_quant_rows_gather(x, T, K, row_token, M, K, fmt_x, flags, ws + p.xq, pitch(K), sx, st));
+    FP8_TRY(fp8k::launch_gemm_fp8_grouped_rows({ws + p.xq, pitch(K), fmt_x, sx, wq, ldw, fmt_w, scale_w, offsets, E, M, N, K, y, N}, st));
+    return FP8_OK;
+}
+
+int fp8_adamw_step(const fp8_adamw_tensor* tensors, int64_t count, int flags, double lr, double beta1, double beta2, double eps,
+                   double weight_decay, int64_t step, const float* grad_scale, void* stream) {
+    const char* fn = "fp8_adamw_step";
+    api_error(FP8_OK, "");
+    if (flags & ~(FP8_ADAMW_PARAM_FP32 | FP8_ADAMW_GRAD_FP32 | FP8_ADAMW_STATE_FP8)) return fail(FP8_ERR_ENUM, "%s: flags=%d has unknown bits", fn, flags);
+    if (count < 0) return fail(FP8_ERR_SHAPE, "%s: count=%lld is negative", fn, (ll)count);
+    if (!(lr >= 0) || !(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1) || !(eps >= 0) || !(weight_decay >= 0) || step < 1)
+        return fail(FP8_ERR_SHAPE, "%s: lr=%g betas=(%g, %g) eps=%g weight_decay=%g step=%lld out of range", fn, lr, beta1, beta2, eps, weight_decay, (ll)step);
+    if (!aligned(grad_scale, 4)) return fail(FP8_ERR_ALIGN, "%s: grad_scale not 4-byte aligned", fn);
+    if (count == 0) return FP8_OK;
+    if (!tensors) return fail(FP8_ERR_NULL, "%s: tensors is NULL", fn);
+    const bool q = flags & FP8_ADAMW_STATE_FP8;
+    for (int64_t i = 0; i < count; ++i) {
+        const fp8_adamw_tensor& t = tensors[i];
+        if (t.n < 0) return fail(FP8_ERR_SHAPE, "%s: tensor %lld has n=%lld", fn, (ll)i, (ll)t.n);
+        if (t.n == 0) continue;
+        if (!t.param || !t.grad || !t.exp_avg || !t.exp_avg_sq || (q && (!t.scale_m || !t.scale_v)))
+            return fail(FP8_ERR_NULL, "%s: tensor %lld has a NULL pointer", fn, (ll)i);
+        if (!aligned(t.param, 16) || !aligned(t.grad, 16) || !aligned(t.exp_avg, 16) || !aligned(t.exp_avg_sq, 16) ||
+            (q && (!aligned(t.scale_m, 4) || !aligned(t.scale_v, 4))))
+            return fail(FP8_ERR_ALIGN, "%s: tensor %lld: a pointer is not 16-byte (scales: 4-byte) aligned", fn, (ll)i);
+    }
+    static_assert(sizeof(fp8_adamw_tensor) == sizeof(fp8k::AdamwTensor), "the same layout");
+    const double bc1 = 1.0 - std::pow(beta1, (double)step), bc2 = 1.0 - std::pow(beta2, (double)step);
+    const fp8k::AdamwScalars s{(float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)(1.0 - lr * weight_decay),
+                               (float)(lr / bc1), (float)(1.0 / std::sqrt(bc2)), (float)eps, grad_scale};
+    FP8_TRY(fp8k::launch_adamw(reinterpret_cast<const fp8k::AdamwTensor*>(tensors), count, flags & FP8_ADAMW_PARAM_FP32, flags & FP8_ADAMW_GRAD_FP32, q,
+                               s, static_cast<hipStream_t>(stream)));
+    return FP8_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,168 @@
+// The outputs of a token's experts put together, and the gradients behind it:
+//   out[t] = sum_j gate[t, j] y[slot_row[t, j]]            (in the order of j, in binary32, rounded once to bfloat16)
+//   dy[slot_row[t, j]] = gate[t, j] dout[t],   dgate[t, j] = sum_d dout[t, d] y[slot_row[t, j], d]
+// A slot without a row (slot_row outside [0, M)) contributes nothing.  gates nullptr: all one, which is the sum that turns the
+// experts' input gradients into the tokens'.
+//
+// Both are bound by HBM: each row of y passes once, k of them for one of the output.
+#include "fp8_device.hpp"
+#include "moe_launchers.hpp"
+
+namespace fp8k {
+
+namespace {
+
+typedef __bf16 bf16x2_c __attribute__((ext_vector_type(2)));
+typedef float f32x2_c __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    const f32x2_c v = {a, b};
+    const bf16x2_c h = __builtin_convertvector(v, bf16x2_c);
+    uint32_t r;
+    __builtin_memcpy(&r, &h, 4);
+    return r;
+}
+__device__ __forceinline__ void widen8(const uint4& v, float (&f)[8]) {
+    f[0] = bf16_lo(v.x); f[1] = bf16_hi(v.x); f[2] = bf16_lo(v.y); f[3] = bf16_hi(v.y);
+    f[4] = bf16_lo(v.z); f[5] = bf16_hi(v.z); f[6] = bf16_lo(v.w); f[7] = bf16_hi(v.w);
+}
+__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
+    return make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
+}
+
+// a thread: eight columns of one token, the rows of four slots under way at a time
+__global__ __launch_bounds__(256) void combine_kernel(const uint16_t* __restrict__ y, int M, int64_t ld, const float* __restrict__ gates,
+                                                      const int32_t* __restrict__ slot_row, int64_t pieces, int per_row, int k,
+                                                      uint16_t* __restrict__ out, int64_t ld_out) {
+    const int64_t piece = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (piece >= pieces) return;
+    const int64_t t = piece / per_row;
+    const int c = (int)(piece - t * per_row) * 8;
+    float sum[8] = {};
+    for (int j0 = 0; j0 < k; j0 += 4) {
+        uint4 v[4];
+        float g[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int j = j0 + i;
+            const int row = j < k ? slot_row[t * k + j] : -1;
+            const bool there = row >= 0 && row < M;
+            g[i] = !there ? 0.f : gates ? gates[t * k + j] : 1.f;
+            v[i] = there ? load_stream(y + row * ld + c) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float f[8];
+            widen8(v[i], f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += g[i] * f[e];
+        }
+    }
+    *reinterpret_cast<uint4*>(out + t * ld_out + c) = pack8(sum);
+}
+
+// A wavefront per token below, else a workgroup: NW wavefronts.  Blocks from `tokens` on clear the rows that belong to no token.
+template <int NW>
+__global__ __launch_bounds__(64 * NW) void combine_bwd_kernel(const uint16_t* __restrict__ dout, int64_t ld_dout, const uint16_t* __restrict__ y,
+                                                              int64_t ld, const float* __restrict__ gates, const int32_t* __restrict__ slot_row,
+                                                              const int32_t* __restrict__ row_token, int M, int T, int D, int k,
+                                                              uint16_t* __restrict__ dy, int64_t ld_dy, float* __restrict__ dgates) {
+    constexpr int NTH = 64 * NW, KEPT = 4;       // pieces of dout that stay in registers from slot to slot
+    __shared__ float part[NW];
+    const int tid = threadIdx.x;
+    if ((int)blockIdx.x >= T) {
+        const int r0 = ((int)blockIdx.x - T) * 64, r1 = r0 + 64 < M ? r0 + 64 : M;
+        for (int r = r0; r < r1; ++r) {
+            const int t = row_token[r];
+            if (t >= 0 && t < T) continue;
+            for (int c = tid * 8; c < D; c += NTH * 8) *reinterpret_cast<uint4*>(dy + r * ld_dy + c) = make_uint4(0, 0, 0, 0);
+        }
+        return;
+    }
+    const int64_t t = blockIdx.x;
+    uint4 kept[KEPT];
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) {
+        const int c = (i * NTH + tid) * 8;
+        kept[i] = c < D ? *reinterpret_cast<const uint4*>(dout + t * ld_dout + c) : make_uint4(0, 0, 0, 0);
+    }
+    for (int j = 0; j < k; ++j) {
+        const int row = slot_row[t * k + j];
+        const bool there = row >= 0 && row < M;
+        const float g = there && gates ? gates[t * k + j] : 1.f;
+        float sum = 0.f;
+        auto piece = [&](const uint4& d4, const uint4& y4, int c) {
+            float d[8], o[8];
+            widen8(d4, d);
+            if (dgates) {
+                float f[8];
+                widen8(y4, f);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum += d[e] * f[e];
+            }
+            if (dy) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = g * d[e];
+                *reinterpret_cast<uint4*>(dy + row * ld_dy + c) = pack8(o);
+            }
+        };
+        if (there) {
+            uint4 v[KEPT];
+#pragma unroll
+            for (int i = 0; i < KEPT; ++i) {
+                const int c = (i * NTH + tid) * 8;
+                v[i] = dgates && c < D ? load_stream(y + row * ld + c) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < KEPT; ++i) {
+                const int c = (i * NTH + tid) * 8;
+                if (c < D) piece(kept[i], v[i], c);
+            }
+            for (int c = (KEPT * NTH + tid) * 8; c < D; c += NTH * 8)
+                piece(*reinterpret_cast<const uint4*>(dout + t * ld_dout + c), dgates ? load_stream(y + row * ld + c) : make_uint4(0, 0, 0, 0), c);
+        }
+        if (dgates) {
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+            if constexpr (NW == 1) {
+                if (tid == 0) dgates[t * k + j] = sum;
+            } else {
+                if ((tid & 63) == 0) part[tid >> 6] = sum;
+                __syncthreads();
+                if (tid == 0) {
+                    float s = part[0];
+#pragma unroll
+                    for (int w = 1; w < NW; ++w) s += part[w];
+                    dgates[t * k + j] = s;
+                }
+                __syncthreads();
+            }
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_moe_combine(const void* y, int64_t M, int64_t ld, const float* gates, const int32_t* slot_row, int64_t T, int64_t D, int k,
+                              void* out, int64_t ld_out, hipStream_t st) {
+    const int64_t pieces = T * (D / 8);
+    combine_kernel<<<(unsigned)((pieces + 255) / 256), 256, 0, st>>>(static_cast<const uint16_t*>(y), (int)M, ld, gates, slot_row, pieces,
+                                                                     (int)(D / 8), k, static_cast<uint16_t*>(out), ld_out);
+    return hipGetLastError();
+}
+
+hipError_t launch_moe_combine_bwd(const void* dout, int64_t ld_dout, const void* y, int64_t ld, const float* gates, const int32_t* slot_row,
+                                  const int32_t* row_token, int64_t M, int64_t T, int64_t D, int k, void* dy, int64_t ld_dy, float* dgates,
+                                  hipStream_t st) {
+    const unsigned grid = (unsigned)(T + (dy ? (M + 63) / 64 : 0));
+#define FP8K_BWD(NW_)                                                                                                                        \
+    combine_bwd_kernel<NW_><<<grid, 64 * NW_, 0, st>>>(static_cast<const uint16_t*>(dout), ld_dout, static_cast<const uint16_t*>(y), ld, gates, \
+                                                       slot_row, row_token, (int)M, (int)T, (int)D, k, static_cast<uint16_t*>(dy), ld_dy, dgates)
+    if (D <= 1024) FP8K_BWD(1);
+    else if (D <= 4096) FP8K_BWD(2);
+    else FP8K_BWD(4);
+#undef FP8K_BWD
+    return hipGetLastError();
+}
+
+}  // namespace fp8k

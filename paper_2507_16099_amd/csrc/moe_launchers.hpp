@@ -1,0 +1,62 @@
+// Launch functions of the mixture-of-experts operators and of the AdamW step (moe_api.hip calls them).  Arguments are assumed valid
+// (the ABI layer checks them); every function only enqueues work on `st`.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace fp8k {
+
+// the description of the last error on the calling thread, as fp8_last_error returns it (api.hip); gives code back
+int api_error(int code, const char* text);
+
+// ---- router (moe_route.hip)
+constexpr int ROUTE_MAX_EXPERTS = 512;
+constexpr int ROUTE_MAX_K = 16;
+size_t route_workspace_bytes(int64_t T, int64_t E);
+hipError_t launch_moe_route(const void* logits, bool f32, int64_t T, int64_t E, int64_t ld, int k, bool renorm, float* gates, int32_t* experts,
+                            int32_t* offsets, int32_t* row_token, int32_t* slot_row, void* ws, hipStream_t st);
+hipError_t launch_moe_route_bwd(const float* dgates, const void* logits, bool f32, int64_t T, int64_t E, int64_t ld, int k, bool renorm,
+                                const float* gates, const int32_t* experts, void* dlogits, int64_t ld_out, hipStream_t st);
+
+// ---- combination of the experts' outputs (moe_combine.hip)
+hipError_t launch_moe_combine(const void* y, int64_t M, int64_t ld, const float* gates, const int32_t* slot_row, int64_t T, int64_t D, int k,
+                              void* out, int64_t ld_out, hipStream_t st);
+hipError_t launch_moe_combine_bwd(const void* dout, int64_t ld_dout, const void* y, int64_t ld, const float* gates, const int32_t* slot_row,
+                                  const int32_t* row_token, int64_t M, int64_t T, int64_t D, int k, void* dy, int64_t ld_dy, float* dgates,
+                                  hipStream_t st);
+
+// ---- quantization of grouped operands (grouped_quant.hip)
+// rows x[row_token[r]] (row_token nullptr: x[r]) -> codes q [M, ld_q] and scales [M]; a row whose token is not in [0, T) is a row of zeros
+hipError_t launch_quant_rows_gather(const void* x, int64_t T, int64_t ldx, const int32_t* row_token, int64_t M, int64_t cols, int fmt, int flags,
+                                    uint8_t* q, int64_t ld_q, float* scale, hipStream_t st);
+// One operand quantized per column within each group of rows and written transposed.
+//   rows of group e: offsets given: [offsets[e], offsets[e + 1]) of the M rows, else [e M / E, (e + 1) M / E) (M a multiple of E)
+//   qt: with offsets [cols, ld_t], the codes of a group start at the sum of the earlier groups' lengths, each padded to 128, and
+//   zero codes follow up to the next 16; else [E, cols, ld_t].  scale [E, cols]; amax [E, cols]: scratch
+struct GroupedColOperand {
+    const void* x; int64_t T, ldx; const int32_t* row_token; int64_t M, cols; int fmt;
+    uint8_t* qt; int64_t ld_t; float* scale; uint32_t* amax;
+};
+hipError_t launch_quant_cols_grouped(const GroupedColOperand& op, const int32_t* offsets, int64_t E, int flags, hipStream_t st);
+// columns that the padded groups of M rows can come to
+inline int64_t grouped_padded(int64_t M, int64_t E) { return (M + 127 * (E < M ? E : M) + 127) / 128 * 128; }
+
+// ---- products grouped by expert (gemm_fp8_grouped.hip): out = A B^T / (scale_a scale_b), operands as for launch_gemm_fp8
+struct GroupedGemm {
+    const uint8_t* a; int64_t lda; int fmt_a; const float* scale_a;
+    const uint8_t* b; int64_t ldb; int fmt_b; const float* scale_b;
+    const int32_t* offsets; int64_t E, M, N, K;
+    void* out; int64_t ld_out;
+};
+// out[r, :N] for the rows r of a group: A row r [K], B rows of that group (b + e N ldb, scale_b + e N); rows past the last group: zeros
+hipError_t launch_gemm_fp8_grouped_rows(const GroupedGemm& g, hipStream_t st);
+// out[e] [N, K] for each group: A [N, lda], B [K, ldb] with the group's columns where launch_quant_cols_grouped leaves them;
+// scale_a [E, N], scale_b [E, K]
+hipError_t launch_gemm_fp8_grouped_contract(const GroupedGemm& g, hipStream_t st);
+
+// ---- AdamW (adamw.hip)
+struct AdamwTensor { void* p; const void* g; void *m, *v; float *sm, *sv; int64_t n; };
+struct AdamwScalars { float b1, c1, b2, c2, decay, rate, inv_root, eps; const float* grad_scale; };
+hipError_t launch_adamw(const AdamwTensor* tensors, int64_t count, bool p_f32, bool g_f32, bool fp8_state, const AdamwScalars& s, hipStream_t st);
+
+}  // namespace fp8k

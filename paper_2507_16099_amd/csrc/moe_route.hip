@@ -1,0 +1,354 @@
+// The router of a mixture-of-experts layer: which k of E experts each token goes to, with which gates, and the expert-ordered row
+// lists that the grouped products read; and the gradient of the logits.
+//
+//   p = softmax(l), S = the k largest logits (ties to the lower expert; -inf and NaN are never chosen)
+//   gate_j = p_j, or p_j / sum over S with renormalisation: e^(l_j - max) / (sum over all, or over S)
+//   rows: the slots (t, j) that have an expert, in the order of (expert, t, j)
+//
+// Choice: LANES lanes hold a token's logits, VPL each, as unsigned integers that order like the values (0: not to be chosen).  A
+// round takes their maximum and the lowest expert that has it: k rounds of a register reduction and a ballot.
+// Lists: a chunk of consecutive tokens per workgroup.  The first launch leaves each chunk's count per expert; the second adds up
+// what lies before its chunk and ranks its own slots, 64 at a time: lanes with the same expert find each other with one ballot per
+// bit of the expert's number, so ranks, and the lists, come out in order and alike every time, without atomics on positions.
+// A few tokens (one chunk) take one launch.
+//
+// Bound: 16 tokens of 64 experts are a launch's latency; 16384 tokens of 64 experts read 4 MB and write 1.6 MB, far less than what
+// the rounds and the two launches take.
+#include "moe_launchers.hpp"
+
+namespace fp8k {
+
+namespace {
+
+constexpr int NT = 1024;                 // threads of a route workgroup
+constexpr int MAX_CHUNKS = 256;
+
+__device__ __forceinline__ float load_logit(const void* p, bool f32, int64_t i) {
+    if (f32) return static_cast<const float*>(p)[i];
+    return __uint_as_float((uint32_t) static_cast<const uint16_t*>(p)[i] << 16);
+}
+
+// order of the values as unsigned integers; -0 as 0; -inf and NaN as 0, below everything
+__device__ __forceinline__ uint32_t order_of(float x) {
+    if (!(x > -__builtin_inff())) return 0u;
+    const uint32_t b = __float_as_uint(x + 0.0f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o); }
+
+template <int LANES>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
+#pragma unroll
+    for (int d = LANES / 2; d > 0; d >>= 1) {
+        const uint32_t o = (uint32_t)__shfl_xor((int)v, d, 64);
+        v = o > v ? o : v;
+    }
+    return v;
+}
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+    for (int d = LANES / 2; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
+    return v;
+}
+
+// the logits of token t in LANES lanes: expert lane + LANES i
+template <int LANES, int VPL>
+__device__ __forceinline__ void load_token(const void* logits, bool f32, int64_t t, int64_t ld, int E, int l, float (&x)[VPL]) {
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+        const int e = l + LANES * i;
+        x[i] = e < E ? load_logit(logits, f32, t * ld + e) : -__builtin_inff();
+    }
+}
+
+struct RouteArgs {
+    const void* logits;
+    int f32, T, E, k, renorm, chunk;     // chunk: tokens per workgroup
+    int64_t ld;
+    float* gates;
+    int32_t *experts, *offsets, *row_token, *slot_row;
+    int32_t* counts;                     // [chunks, E]
+};
+
+// experts and gates of the chunk's tokens, and how many slots each expert got in hist[E]
+template <int LANES, int VPL>
+__device__ void choose(const RouteArgs& a, int t0, int t1, int* hist) {
+    const int l = threadIdx.x % LANES, sub = threadIdx.x / LANES;
+    const int first_lane = (threadIdx.x & 63) - l;
+    const uint64_t mine = (LANES == 64 ? ~0ull : (1ull << (LANES & 63)) - 1) << first_lane;
+    for (int tb = t0; tb < t1; tb += NT / LANES) {
+        const int t = tb + sub;
+        const bool live = t < t1;
+        float x[VPL];
+        load_token<LANES, VPL>(a.logits, a.f32, live ? t : t1 - 1, a.ld, a.E, l, x);
+        uint32_t o[VPL];
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) o[i] = order_of(x[i]);
+        float top = 0.f, my_value = 0.f, all = 0.f;
+        int my_expert = -1;
+        for (int j = 0; j < a.k; ++j) {
+            uint32_t best = o[0];
+#pragma unroll
+            for (int i = 1; i < VPL; ++i) best = o[i] > best ? o[i] : best;
+            best = lanes_max<LANES>(best);
+            int expert = -1;
+#pragma unroll
+            for (int i = VPL - 1; i >= 0; --i) {
+                const uint64_t has = __ballot(best != 0 && o[i] == best) & mine;
+                if (has) expert = LANES * i + __ffsll((unsigned long long)has) - 1 - first_lane;
+            }
+#pragma unroll
+            for (int i = 0; i < VPL; ++i)
+                if (expert == l + LANES * i) o[i] = 0u;
+            if (j == 0) {
+                top = best ? value_of(best) : 0.f;
+                float s = 0.f;
+#pragma unroll
+                for (int i = 0; i < VPL; ++i) s += l + LANES * i < a.E ? expf(x[i] - top) : 0.f;
+                all = lanes_sum<LANES>(s);
+            }
+            if (l == j) {      // (k <= ROUTE_MAX_K <= LANES)
+                my_value = best ? value_of(best) : 0.f;
+                my_expert = expert;
+            }
+        }
+        float e = my_expert >= 0 ? expf(my_value - top) : 0.f;
+        const float total = a.renorm ? lanes_sum<LANES>(l < a.k ? e : 0.f) : all;
+        if (live && l < a.k) {
+            const int64_t s = (int64_t)t * a.k + l;
+            a.experts[s] = my_expert;
+            a.gates[s] = my_expert < 0 ? 0.f : e / total;
+            if (my_expert >= 0) atomicAdd(&hist[my_expert], 1);
+        }
+    }
+}
+
+// the chunk's slots to their places; base[E]: where the first slot of each expert goes.  hist: [16][E] scratch, one row per wavefront
+__device__ void place(const RouteArgs& a, int64_t s0, int64_t s1, const int* base, int* hist) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int E = a.E;
+    const int64_t part = ((s1 - s0 + 15) / 16 + 63) / 64 * 64;      // slots of a wavefront, whole sixty-fours
+    const int64_t w0 = s0 + wave * part < s1 ? s0 + wave * part : s1, w1 = w0 + part < s1 ? w0 + part : s1;
+    for (int i = threadIdx.x; i < 16 * E; i += NT) hist[i] = 0;
+    __syncthreads();
+    for (int64_t s = w0 + lane; s < w1; s += 64) {
+        const int e = a.experts[s];
+        if (e >= 0) atomicAdd(&hist[wave * E + e], 1);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += NT) {
+        int at = base[e];
+        for (int w = 0; w < 16; ++w) {
+            const int n = hist[w * E + e];
+            hist[w * E + e] = at;
+            at += n;
+        }
+    }
+    __syncthreads();
+    int* next = hist + wave * E;
+    for (int64_t sb = w0; sb < w1; sb += 64) {
+        const int64_t s = sb + lane;
+        const int e = s < w1 ? a.experts[s] : -1;
+        uint64_t same = __ballot(e >= 0);
+        for (int bit = 0; (1 << bit) < E; ++bit) {
+            const uint64_t m = __ballot((e >> bit) & 1);
+            same &= (e >> bit) & 1 ? m : ~m;
+        }
+        const int before = __popcll(same & ((1ull << lane) - 1));
+        int row = -1;
+        if (e >= 0) row = next[e] + before;
+        // (the reads above are done by the whole wavefront before the first lane of each expert moves its count on)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        if (e >= 0 && before == 0) next[e] += __popcll(same);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        if (s < w1) {
+            a.slot_row[s] = row;
+            if (row >= 0) a.row_token[row] = (int)(s / a.k);
+        }
+    }
+}
+
+// exclusive prefix of n <= ROUTE_MAX_EXPERTS counts in LDS, by the first wavefront; out[n] the sum
+__device__ void prefix(const int* counts, int* out, int n) {
+    if (threadIdx.x < 64) {
+        const int lane = threadIdx.x;
+        int before = 0;
+        for (int e0 = 0; e0 < n; e0 += 64) {
+            const int c = e0 + lane < n ? counts[e0 + lane] : 0;
+            int v = c;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int o = __shfl_up(v, d, 64);
+                if (lane >= d) v += o;
+            }
+            if (e0 + lane < n) out[e0 + lane] = before + v - c;
+            before += __shfl(v, 63, 64);
+        }
+        if (lane == 0) out[n] = before;
+    }
+}
+
+// ONE: the only chunk - choice and lists in one launch.  Else the choice and the chunk's counts.
+template <int LANES, int VPL, bool ONE>
+__global__ __launch_bounds__(NT) void route_choose_kernel(RouteArgs a) {
+    extern __shared__ int smem[];        // counts [E], base [E + 1], hist [16][E]
+    int *counts = smem, *base = smem + a.E, *hist = base + a.E + 1;
+    for (int e = threadIdx.x; e < a.E; e += NT) counts[e] = 0;
+    __syncthreads();
+    const int t0 = blockIdx.x * a.chunk, t1 = t0 + a.chunk < a.T ? t0 + a.chunk : a.T;
+    choose<LANES, VPL>(a, t0, t1, counts);
+    __syncthreads();                     // (also makes the experts that this workgroup wrote readable to all of it)
+    if constexpr (!ONE) {
+        for (int e = threadIdx.x; e < a.E; e += NT) a.counts[(int64_t)blockIdx.x * a.E + e] = counts[e];
+    } else {
+        prefix(counts, base, a.E);
+        __syncthreads();
+        for (int e = threadIdx.x; e <= a.E; e += NT) a.offsets[e] = base[e];
+        const int64_t S = (int64_t)a.T * a.k;
+        for (int64_t r = base[a.E] + threadIdx.x; r < S; r += NT) a.row_token[r] = -1;
+        place(a, 0, S, base, hist);
+    }
+}
+
+__global__ __launch_bounds__(NT) void route_place_kernel(RouteArgs a) {
+    extern __shared__ int smem[];        // all [E], before [E], base [E + 1], hist [16][E]
+    int *all = smem, *before = smem + a.E, *base = before + a.E, *hist = base + a.E + 1;
+    const int chunks = gridDim.x, b = blockIdx.x;
+    for (int e = threadIdx.x; e < 2 * a.E; e += NT) smem[e] = 0;
+    __syncthreads();
+    {
+        // counts of all chunks and of those before this one: NT / E chunks at a time
+        const int lanes = a.E < NT ? a.E : NT, groups = NT / lanes, g = threadIdx.x / lanes, l = threadIdx.x % lanes;
+        if (g < groups) {
+            int sum = 0, sum_before = 0;
+            for (int c = g; c < chunks; c += groups) {
+                const int n = a.counts[(int64_t)c * a.E + l];
+                sum += n;
+                if (c < b) sum_before += n;
+            }
+            atomicAdd(&all[l], sum);
+            atomicAdd(&before[l], sum_before);
+        }
+    }
+    __syncthreads();
+    prefix(all, base, a.E);
+    __syncthreads();
+    const int64_t S = (int64_t)a.T * a.k;
+    const int used = base[a.E];
+    if (b == 0)
+        for (int e = threadIdx.x; e <= a.E; e += NT) a.offsets[e] = base[e];
+    for (int64_t r = used + (int64_t)b * NT + threadIdx.x; r < S; r += (int64_t)chunks * NT) a.row_token[r] = -1;
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.E; e += NT) base[e] += before[e];
+    __syncthreads();
+    const int64_t s0 = (int64_t)b * a.chunk * a.k, s1 = s0 + (int64_t)a.chunk * a.k;
+    place(a, s0 < S ? s0 : S, s1 < S ? s1 : S, base, hist);
+}
+
+// dl = p (dg - sum_S g dg) over the experts, dg = 0 outside S; with renormalisation g (dg - sum_S g dg) on S, else 0
+template <int LANES, int VPL>
+__global__ __launch_bounds__(256) void route_bwd_kernel(const float* __restrict__ dgates, const void* __restrict__ logits, int f32, int T, int E,
+                                                        int64_t ld, int k, int renorm, const float* __restrict__ gates,
+                                                        const int32_t* __restrict__ experts, void* __restrict__ dlogits, int64_t ld_out) {
+    const int l = threadIdx.x % LANES;
+    const int t = (int)(blockIdx.x * (256 / LANES) + threadIdx.x / LANES);
+    const bool live = t < T;
+    const int64_t tt = live ? t : T - 1;
+    // slots of the token in its first k lanes (LANES >= k)
+    const int my_expert = l < k ? experts[tt * k + l] : -1;
+    const float g = my_expert >= 0 ? gates[tt * k + l] : 0.f, dg = my_expert >= 0 ? dgates[tt * k + l] : 0.f;
+    const float inner = lanes_sum<LANES>(g * dg);
+    float d[VPL];
+    if (renorm) {
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) d[i] = 0.f;
+    } else {
+        float x[VPL];
+        load_token<LANES, VPL>(logits, f32, tt, ld, E, l, x);
+        uint32_t o = 0;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) { const uint32_t oi = order_of(x[i]); o = oi > o ? oi : o; }
+        o = lanes_max<LANES>(o);
+        const float top = o ? value_of(o) : 0.f;
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) {
+            x[i] = l + LANES * i < E ? expf(x[i] - top) : 0.f;
+            s += x[i];
+        }
+        const float total = lanes_sum<LANES>(s);
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) d[i] = o ? -(x[i] / total) * inner : 0.f;
+    }
+    const float share = renorm ? g * (dg - inner) : g * dg;
+    const int first_lane = (threadIdx.x & 63) - l;
+    for (int j = 0; j < k; ++j) {
+        const int e = __shfl(my_expert, first_lane + j, 64);
+        const float v = __shfl(share, first_lane + j, 64);
+#pragma unroll
+        for (int i = 0; i < VPL; ++i)
+            if (e == l + LANES * i) d[i] += v;
+    }
+    if (!live) return;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+        const int e = l + LANES * i;
+        if (e < E) {
+            if (f32) static_cast<float*>(dlogits)[tt * ld_out + e] = d[i];
+            else static_cast<__bf16*>(dlogits)[tt * ld_out + e] = (__bf16)d[i];
+        }
+    }
+}
+
+int64_t chunk_of(int64_t T) { return (T + MAX_CHUNKS - 1) / MAX_CHUNKS; }
+
+}  // namespace
+
+// tokens that one workgroup takes by itself
+static bool one_chunk(int64_t T) { return T <= 64; }
+
+size_t route_workspace_bytes(int64_t T, int64_t E) { return one_chunk(T) ? 256 : (size_t)MAX_CHUNKS * (size_t)E * 4; }
+
+#define FP8K_ROUTE_FORMS(E_, CALL)          \
+    if (E_ <= 16) { CALL(16, 1); }          \
+    else if (E_ <= 32) { CALL(32, 1); }     \
+    else if (E_ <= 64) { CALL(64, 1); }     \
+    else if (E_ <= 128) { CALL(64, 2); }    \
+    else if (E_ <= 256) { CALL(64, 4); }    \
+    else { CALL(64, 8); }
+
+hipError_t launch_moe_route(const void* logits, bool f32, int64_t T, int64_t E, int64_t ld, int k, bool renorm, float* gates, int32_t* experts,
+                            int32_t* offsets, int32_t* row_token, int32_t* slot_row, void* ws, hipStream_t st) {
+    RouteArgs a{logits, f32, (int)T, (int)E, k, renorm, 0, ld, gates, experts, offsets, row_token, slot_row, static_cast<int32_t*>(ws)};
+    const int lds = (int)(20 * E + 1) * 4;
+    if (one_chunk(T)) {
+        a.chunk = (int)T;
+#define FP8K_CALL(L_, V_) route_choose_kernel<L_, V_, true><<<1, NT, lds, st>>>(a)
+        FP8K_ROUTE_FORMS(E, FP8K_CALL)
+#undef FP8K_CALL
+        return hipGetLastError();
+    }
+    a.chunk = (int)chunk_of(T);
+    const unsigned chunks = (unsigned)((T + a.chunk - 1) / a.chunk);
+#define FP8K_CALL(L_, V_) route_choose_kernel<L_, V_, false><<<chunks, NT, lds, st>>>(a)
+    FP8K_ROUTE_FORMS(E, FP8K_CALL)
+#undef FP8K_CALL
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    route_place_kernel<<<chunks, NT, lds, st>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_moe_route_bwd(const float* dgates, const void* logits, bool f32, int64_t T, int64_t E, int64_t ld, int k, bool renorm,
+                                const float* gates, const int32_t* experts, void* dlogits, int64_t ld_out, hipStream_t st) {
+#define FP8K_CALL(L_, V_)                                                                                                              \
+    route_bwd_kernel<L_, V_><<<(unsigned)((T + 256 / L_ - 1) / (256 / L_)), 256, 0, st>>>(dgates, logits, f32, (int)T, (int)E, ld, k, \
+                                                                                         renorm, gates, experts, dlogits, ld_out)
+    FP8K_ROUTE_FORMS(E, FP8K_CALL)
+#undef FP8K_CALL
+    return hipGetLastError();
+}
+
+}  // namespace fp8k

@@ -20,6 +20,8 @@ FP8_E4M3FN, FP8_E5M2 = 0, 1
 FP8_TENSOR, FP8_ROW, FP8_COL = 0, 1, 2
 FP8_POW2_SCALE, FP8_TRANSPOSE_OUT, FP8_OUT_FP32, FP8_GRAD_WEIGHT_HP, FP8_SAVE_FOR_BWD = 1, 2, 4, 8, 16
 FP8_EPILOGUE_SIGMOID = 32
+FP8_ROUTE_RENORM, FP8_ROUTE_FP32 = 64, 128
+FP8_ADAMW_PARAM_FP32, FP8_ADAMW_GRAD_FP32, FP8_ADAMW_STATE_FP8 = 256, 512, 1024
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libfp8mi355.so")
@@ -62,6 +64,11 @@ class Fp8Error(RuntimeError):
 
 class _CRecipe(C.Structure):
     _fields_ = [("gran", C.c_int), ("fmt_x", C.c_int), ("fmt_w", C.c_int), ("fmt_dy", C.c_int), ("flags", C.c_int)]
+
+
+class _CAdamwTensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("exp_avg", C.c_void_p), ("exp_avg_sq", C.c_void_p),
+                ("scale_m", C.c_void_p), ("scale_v", C.c_void_p), ("n", C.c_int64)]
 
 
 @dataclass(frozen=True)
@@ -157,10 +164,34 @@ def load_library() -> C.CDLL:
     L.fp8_grad_weight_hp.argtypes = [vp, vp, i64, i64, i64, vp, vp]
     L.fp8_linear_bwd.restype = ci
     L.fp8_linear_bwd.argtypes = [vp, vp, vp, i64, i64, i64, C.POINTER(_CRecipe), vp, vp, vp, C.c_size_t, vp]
+    sz, rp = C.c_size_t, C.POINTER(_CRecipe)
+    L.fp8_moe_route_workspace_bytes.restype = sz
+    L.fp8_moe_route_workspace_bytes.argtypes = [i64, i64, ci]
+    L.fp8_moe_route.restype = ci
+    L.fp8_moe_route.argtypes = [vp, i64, i64, i64, ci, ci, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.fp8_moe_route_bwd.restype = ci
+    L.fp8_moe_route_bwd.argtypes = [vp, vp, i64, i64, i64, ci, ci, vp, vp, vp, i64, vp]
+    L.fp8_moe_combine.restype = ci
+    L.fp8_moe_combine.argtypes = [vp, i64, i64, vp, vp, i64, i64, ci, vp, i64, vp]
+    L.fp8_moe_combine_bwd.restype = ci
+    L.fp8_moe_combine_bwd.argtypes = [vp, i64, vp, i64, i64, vp, vp, vp, i64, i64, ci, vp, i64, vp, vp]
+    L.fp8_grouped_linear_workspace_bytes.restype = sz
+    L.fp8_grouped_linear_workspace_bytes.argtypes = [i64, i64, i64, i64, rp, ci]
+    L.fp8_grouped_linear_fwd.restype = ci
+    L.fp8_grouped_linear_fwd.argtypes = [vp, i64, vp, vp, vp, i64, i64, i64, i64, rp, vp, vp, sz, vp]
+    L.fp8_grouped_linear_bwd.restype = ci
+    L.fp8_grouped_linear_bwd.argtypes = [vp, vp, i64, vp, vp, vp, i64, i64, i64, i64, rp, vp, vp, vp, sz, vp]
+    L.fp8_grouped_linear_prequantized_workspace_bytes.restype = sz
+    L.fp8_grouped_linear_prequantized_workspace_bytes.argtypes = [i64, i64]
+    L.fp8_grouped_linear_fwd_prequantized.restype = ci
+    L.fp8_grouped_linear_fwd_prequantized.argtypes = [vp, i64, vp, ci, ci, vp, i64, ci, vp, vp, i64, i64, i64, i64, vp, vp, sz, vp]
+    L.fp8_adamw_step.restype = ci
+    L.fp8_adamw_step.argtypes = [vp, i64, ci, C.c_double, C.c_double, C.c_double, C.c_double, C.c_double, i64, vp, vp]
     L.fp8_internal_set_knob.restype = ci
     L.fp8_internal_set_knob.argtypes = [C.c_char_p, ci]
     # the calls of a served model's layers, which take less time on the GPU than ctypes needs to make them
-    for name in ("quantize", "scaled_mm", "linear_fwd_prequantized", "linear_fwd_prequantized_static"):
+    for name in ("quantize", "scaled_mm", "linear_fwd_prequantized", "linear_fwd_prequantized_static", "moe_route", "moe_combine",
+                 "grouped_linear_fwd_prequantized"):
         setattr(L, "fast_" + name, _fast(getattr(L, "fp8_" + name)))
     _lib = L
     return L
@@ -697,3 +728,239 @@ def fp8_mx_linear_bwd(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, fmt_dy
                                             _ptr(dx) if need_dx else None, _ptr(dw) if need_dw else None,
                                             _ptr(workspace), workspace.numel(), _stream()))
     return dx, dw
+
+
+# ---- mixture of experts ---------------------------------------------------------------------------------------------
+
+
+def _dense(t: torch.Tensor, shape, dtype, what: str) -> torch.Tensor:
+    assert t.is_cuda and tuple(t.shape) == tuple(shape) and t.dtype == dtype and t.is_contiguous(), \
+        f"{what}: {tuple(t.shape)} {t.dtype}, want dense {tuple(shape)} {dtype} on the GPU"
+    return t
+
+
+def _logits_of(logits: torch.Tensor, flags: int):
+    """(T, E, ld, flags with the logits' type)"""
+    assert logits.dtype in (torch.bfloat16, torch.float32), logits.dtype
+    T, E, ld = _mat(logits, logits.element_size())
+    return T, E, ld, (flags & ~FP8_ROUTE_FP32) | (FP8_ROUTE_FP32 if logits.dtype == torch.float32 else 0)
+
+
+def fp8_moe_route_workspace_bytes(T: int, E: int, k: int) -> int:
+    n = load_library().fp8_moe_route_workspace_bytes(T, E, k)
+    if n == 0:
+        raise Fp8Error(-2, fp8_last_error())
+    return int(n)
+
+
+def fp8_moe_route(logits: torch.Tensor, k: int, flags: int = 0, out=None, workspace: torch.Tensor | None = None):
+    """The k largest of each token's expert logits [T, E] (bfloat16 or float32): (gates [T, k], experts [T, k], offsets [E + 1],
+    row_token [T k], slot_row [T, k]); out: the same five to write into.  flags: FP8_ROUTE_RENORM."""
+    T, E, ld, flags = _logits_of(logits, flags)
+    dev, i32 = logits.device, torch.int32
+    if workspace is None:
+        workspace = torch.empty(fp8_moe_route_workspace_bytes(T, E, k), dtype=torch.uint8, device=dev)
+    if out is None:
+        out = (torch.empty((T, k), dtype=torch.float32, device=dev), torch.empty((T, k), dtype=i32, device=dev),
+               torch.empty(E + 1, dtype=i32, device=dev), torch.empty(T * k, dtype=i32, device=dev),
+               torch.empty((T, k), dtype=i32, device=dev))
+    gates, experts, offsets, row_token, slot_row = out
+    _dense(gates, (T, k), torch.float32, "gates"), _dense(experts, (T, k), i32, "experts"), _dense(offsets, (E + 1,), i32, "offsets")
+    _dense(row_token, (T * k,), i32, "row_token"), _dense(slot_row, (T, k), i32, "slot_row")
+    _check(load_library().fast_moe_route(logits, T, E, ld, k, flags, gates, experts, offsets, row_token, slot_row, workspace,
+                                         workspace.numel(), _stream()))
+    return out
+
+
+def fp8_moe_route_bwd(dgates: torch.Tensor, logits: torch.Tensor, gates: torch.Tensor, experts: torch.Tensor, flags: int = 0,
+                      out: torch.Tensor | None = None) -> torch.Tensor:
+    """The gradient of the logits from the gates' [T, k] and the forward's logits, gates and experts."""
+    T, E, ld, flags = _logits_of(logits, flags)
+    k = gates.shape[1]
+    _dense(dgates, (T, k), torch.float32, "dgates"), _dense(gates, (T, k), torch.float32, "gates"), _dense(experts, (T, k), torch.int32, "experts")
+    if out is None:
+        out = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
+    assert out.shape == (T, E) and out.dtype == logits.dtype
+    _check(load_library().fp8_moe_route_bwd(_ptr(dgates), _ptr(logits), T, E, ld, k, flags, _ptr(gates), _ptr(experts), _ptr(out),
+                                            _mat(out, out.element_size())[2], _stream()))
+    return out
+
+
+def fp8_moe_combine(y: torch.Tensor, gates: torch.Tensor | None, slot_row: torch.Tensor, out: torch.Tensor | None = None) -> torch.Tensor:
+    """out [T, D] = sum_j gates[t, j] y[slot_row[t, j]]; y [M, D] bfloat16; gates None: all one."""
+    M, D, ld = _mat(y, 2)
+    T, k = slot_row.shape
+    _dense(slot_row, (T, k), torch.int32, "slot_row")
+    if gates is not None:
+        _dense(gates, (T, k), torch.float32, "gates")
+    if out is None:
+        out = torch.empty((T, D), dtype=torch.bfloat16, device=y.device)
+    assert out.shape == (T, D)
+    _check(load_library().fast_moe_combine(y, M, ld, gates, slot_row, T, D, k, out, _mat(out, 2)[2], _stream()))
+    return out
+
+
+def fp8_moe_combine_bwd(dout: torch.Tensor, y: torch.Tensor | None, gates: torch.Tensor | None, slot_row: torch.Tensor,
+                        row_token: torch.Tensor | None, dy: torch.Tensor | None = None, dgates: torch.Tensor | None = None,
+                        need_dy: bool = True, need_dgates: bool = True):
+    """(dy [M, D], dgates [T, k]) of fp8_moe_combine; y and row_token are needed for dgates and dy respectively."""
+    Td, D, ld_dout = _mat(dout, 2)
+    T, k = slot_row.shape
+    assert T == Td, (dout.shape, slot_row.shape)
+    _dense(slot_row, (T, k), torch.int32, "slot_row")
+    if gates is not None:
+        _dense(gates, (T, k), torch.float32, "gates")
+    M, ld = T * k, D
+    if need_dgates:
+        M, Dy, ld = _mat(y, 2)
+        assert D == Dy, (dout.shape, y.shape)
+        dgates = torch.empty((T, k), dtype=torch.float32, device=dout.device) if dgates is None else _dense(dgates, (T, k), torch.float32, "dgates")
+    ld_dy = D
+    if need_dy:
+        M = row_token.numel()
+        _dense(row_token, (M,), torch.int32, "row_token")
+        assert y is None or not need_dgates or y.shape[0] == M, (y.shape, row_token.shape)
+        if dy is None:
+            dy = torch.empty((M, D), dtype=torch.bfloat16, device=dout.device)
+        assert dy.shape == (M, D)
+        ld_dy = _mat(dy, 2)[2]
+    dy, dgates = dy if need_dy else None, dgates if need_dgates else None
+    _check(load_library().fp8_moe_combine_bwd(_ptr(dout), ld_dout, _ptr(y) if need_dgates else None, M, ld, _ptr(gates), _ptr(slot_row),
+                                              _ptr(row_token) if need_dy else None, T, D, k, _ptr(dy), ld_dy, _ptr(dgates), _stream()))
+    return dy, dgates
+
+
+def _grouped(x: torch.Tensor, offsets: torch.Tensor, row_token: torch.Tensor | None):
+    """(T, K, E, M) of grouped rows."""
+    T, K, ldx = _mat(x, 2)
+    assert ldx == K or T <= 1, "x must be dense [T, K]"
+    E = offsets.numel() - 1
+    _dense(offsets, (E + 1,), torch.int32, "offsets")
+    M = T
+    if row_token is not None:
+        M = row_token.numel()
+        _dense(row_token, (M,), torch.int32, "row_token")
+    return T, K, E, M
+
+
+def fp8_grouped_linear_workspace_bytes(M: int, E: int, K: int, N: int, recipe: Recipe, bwd: bool) -> int:
+    r = recipe.c()
+    n = load_library().fp8_grouped_linear_workspace_bytes(M, E, K, N, C.byref(r), int(bwd))
+    if n == 0:
+        raise Fp8Error(-2, fp8_last_error())
+    return int(n)
+
+
+def fp8_grouped_linear_fwd(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, recipe: Recipe, row_token: torch.Tensor | None = None,
+                           y: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Y[r] = x[row_token[r]] W[e]^T for the rows r of group e (offsets [E + 1]); w [E, N, K]; rows behind the last group are zero."""
+    T, K, E, M = _grouped(x, offsets, row_token)
+    N = w.shape[1]
+    _dense(w, (E, N, K), torch.bfloat16, "w")
+    if workspace is None:
+        workspace = torch.empty(fp8_grouped_linear_workspace_bytes(M, E, K, N, recipe, False), dtype=torch.uint8, device=x.device)
+    y = torch.empty((M, N), dtype=torch.bfloat16, device=x.device) if y is None else _dense(y, (M, N), torch.bfloat16, "y")
+    r = recipe.c()
+    _check(load_library().fp8_grouped_linear_fwd(_ptr(x), T, _ptr(row_token), _ptr(w), _ptr(offsets), E, M, K, N, C.byref(r), _ptr(y),
+                                                 _ptr(workspace), workspace.numel(), _stream()))
+    return y
+
+
+def fp8_grouped_linear_bwd(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, recipe: Recipe,
+                           row_token: torch.Tensor | None = None, dx: torch.Tensor | None = None, dw: torch.Tensor | None = None,
+                           workspace: torch.Tensor | None = None, need_dx: bool = True, need_dw: bool = True):
+    """(dX [M, K] by row, dW [E, N, K]) of fp8_grouped_linear_fwd."""
+    T, K, E, M = _grouped(x, offsets, row_token)
+    N = w.shape[1]
+    _dense(w, (E, N, K), torch.bfloat16, "w"), _dense(dy, (M, N), torch.bfloat16, "dy")
+    if workspace is None:
+        workspace = torch.empty(fp8_grouped_linear_workspace_bytes(M, E, K, N, recipe, True), dtype=torch.uint8, device=x.device)
+    if need_dx:
+        dx = torch.empty((M, K), dtype=torch.bfloat16, device=x.device) if dx is None else _dense(dx, (M, K), torch.bfloat16, "dx")
+    if need_dw:
+        dw = torch.empty((E, N, K), dtype=torch.bfloat16, device=x.device) if dw is None else _dense(dw, (E, N, K), torch.bfloat16, "dw")
+    dx, dw = dx if need_dx else None, dw if need_dw else None
+    r = recipe.c()
+    _check(load_library().fp8_grouped_linear_bwd(_ptr(dy), _ptr(x), T, _ptr(row_token), _ptr(w), _ptr(offsets), E, M, K, N, C.byref(r),
+                                                 _ptr(dx), _ptr(dw), _ptr(workspace), workspace.numel(), _stream()))
+    return dx, dw
+
+
+def fp8_grouped_linear_prequantized_workspace_bytes(M: int, K: int) -> int:
+    n = load_library().fp8_grouped_linear_prequantized_workspace_bytes(M, K)
+    if n == 0:
+        raise Fp8Error(-2, fp8_last_error())
+    return int(n)
+
+
+def fp8_grouped_linear_fwd_prequantized(x: torch.Tensor, wq: torch.Tensor, fmt_w: int, scale_w: torch.Tensor, offsets: torch.Tensor,
+                                        fmt_x: int = FP8_E4M3FN, flags: int = 0, row_token: torch.Tensor | None = None,
+                                        y: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """fp8_grouped_linear_fwd with weights quantized beforehand: codes wq [E, N, K] (fp8_quantize of [E N, K] by row, viewed) and
+    scales scale_w [E, N]."""
+    T, K, E, M = _grouped(x, offsets, row_token)
+    N = wq.shape[1]
+    assert wq.is_cuda and tuple(wq.shape) == (E, N, K) and wq.element_size() == 1 and wq.stride(2) == 1, (wq.shape, wq.dtype)
+    ldw = wq.stride(1) if N > 1 else wq.stride(0)
+    assert E == 1 or wq.stride(0) == N * ldw, "the experts' codes must lie one behind the other"
+    _dense(scale_w, (E, N), torch.float32, "scale_w")
+    if workspace is None:
+        workspace = torch.empty(fp8_grouped_linear_prequantized_workspace_bytes(M, K), dtype=torch.uint8, device=x.device)
+    y = torch.empty((M, N), dtype=torch.bfloat16, device=x.device) if y is None else _dense(y, (M, N), torch.bfloat16, "y")
+    _check(load_library().fast_grouped_linear_fwd_prequantized(x, T, row_token, fmt_x, flags, wq, ldw, fmt_w, scale_w, offsets, E, M, K, N, y,
+                                                               workspace, workspace.numel(), _stream()))
+    return y
+
+
+# ---- AdamW ----------------------------------------------------------------------------------------------------------
+
+FP8_ADAMW_BLOCK = 256
+
+
+class AdamwTensors:
+    """The tensors of an AdamW step as the library reads them; made once, kept with the parameters (and keeps them)."""
+
+    def __init__(self, array, count: int, flags: int, tensors):
+        self.array, self.count, self.flags, self.tensors = array, count, flags, tensors
+
+
+def fp8_adamw_tensors(params, grads, exp_avg, exp_avg_sq, scale_m=None, scale_v=None) -> AdamwTensors:
+    """Lists of dense tensors, one entry per parameter; params and grads in bfloat16 or float32 (alike in each list).  Moments in
+    float32, or as e4m3 codes (uint8) with scale_m / scale_v: one power-of-two scale per FP8_ADAMW_BLOCK elements, of exp_avg_sq
+    for the codes of its square root."""
+    def kind(ts, allowed, what):
+        kinds = {t.dtype for t in ts}
+        assert len(kinds) <= 1 and kinds <= set(allowed), f"{what}: {kinds}"
+        return kinds.pop() if kinds else allowed[0]
+
+    both = (torch.bfloat16, torch.float32)
+    lists = [list(ts) for ts in (params, grads, exp_avg, exp_avg_sq)]
+    n = len(lists[0])
+    flags = FP8_ADAMW_PARAM_FP32 if kind(lists[0], both, "params") == torch.float32 else 0
+    flags |= FP8_ADAMW_GRAD_FP32 if kind(lists[1], both, "grads") == torch.float32 else 0
+    states = (torch.float32, torch.uint8)
+    of_m, of_v = kind(lists[2], states, "exp_avg"), kind(lists[3], states, "exp_avg_sq")
+    assert of_m == of_v, (of_m, of_v)
+    if of_m == torch.uint8:
+        flags |= FP8_ADAMW_STATE_FP8
+        assert scale_m is not None and scale_v is not None, "8-bit moments come with scales"
+        lists += [list(scale_m), list(scale_v)]
+        kind(lists[4], (torch.float32,), "scale_m"), kind(lists[5], (torch.float32,), "scale_v")
+    assert all(len(ts) == n for ts in lists), [len(ts) for ts in lists]
+    array = (_CAdamwTensor * max(n, 1))()
+    for i, ts in enumerate(zip(*lists)):
+        size = ts[0].numel()
+        assert all(t.is_cuda and t.is_contiguous() for t in ts), f"tensor {i}: not dense on the GPU"
+        assert all(t.numel() == size for t in ts[:4]) and all(t.numel() == -(-size // FP8_ADAMW_BLOCK) for t in ts[4:]), \
+            f"tensor {i}: sizes {[t.numel() for t in ts]}"
+        ptrs = [t.data_ptr() if size else None for t in ts] + [None] * (6 - len(ts))
+        array[i] = _CAdamwTensor(*ptrs, size)
+    return AdamwTensors(array, n, flags, lists)
+
+
+def fp8_adamw_step(tensors: AdamwTensors, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                   weight_decay: float = 0.01, grad_scale: torch.Tensor | None = None) -> None:
+    """One AdamW step in place over all of them.  grad_scale: one float32 on the GPU that multiplies the gradients."""
+    assert grad_scale is None or (grad_scale.is_cuda and grad_scale.dtype == torch.float32 and grad_scale.numel() == 1)
+    _check(load_library().fp8_adamw_step(C.addressof(tensors.array), tensors.count, tensors.flags, lr, beta1, beta2, eps, weight_decay, step,
+                                         _ptr(grad_scale), _stream()))
