@@ -33,14 +33,17 @@ static_assert(sizeof(Many) + sizeof(AdamwScalars) <= 4096, "kernel arguments");
 struct Update {
     AdamwScalars s;
     float c;
+    // (no contraction: moments that come from four-bit codes fall on ties between codes, where a product left unrounded decides)
     __device__ __forceinline__ void moments(float g, float& m, float& v) const {
-        g = __fmul_rn(g, c);
-        m = __fadd_rn(__fmul_rn(m, s.b1), __fmul_rn(g, s.c1));
-        v = __fadd_rn(__fmul_rn(v, s.b2), __fmul_rn(__fmul_rn(g, g), s.c2));
+#pragma clang fp contract(off)
+        g = g * c;
+        m = m * s.b1 + g * s.c1;
+        v = v * s.b2 + (g * g) * s.c2;
     }
     __device__ __forceinline__ float param(float p, float m, float root) const {
-        const float d = __fadd_rn(__fmul_rn(root, s.inv_root), s.eps);
-        return __fsub_rn(__fmul_rn(p, s.decay), __fmul_rn(__fdiv_rn(m, d), s.rate));
+#pragma clang fp contract(off)
+        const float d = root * s.inv_root + s.eps;
+        return p * s.decay - __fdiv_rn(m, d) * s.rate;
     }
 };
 
@@ -165,7 +168,7 @@ __global__ __launch_bounds__(NT) void adamw_kernel(Many many, AdamwScalars s) {
             for (int e = 0; e < 8; ++e) {
                 m[e] *= inv_m;
                 const float ro = root[e] * inv_v;
-                v[e] = __fmul_rn(ro, ro);
+                v[e] = ro * ro;      // (eight significant bits: exact)
             }
         } else {
             load8(static_cast<const float*>(t.m) + i, n, m);
