@@ -527,10 +527,14 @@ int fp8_grouped_linear_fwd_prequantized(const void* x, int64_t T, const int32_t*
  * exp_avg_sq = sqrt(v) * scale_v with one power-of-two scale per block, [(n + 255) / 256]
  * each; a nonzero root is never rounded to zero.  To start, codes of zero with any
  * power-of-two scales.  This step's update uses the moments before that rounding.
- * tensors: an array in HOST memory of count descriptors, read before the call returns;
- * its pointers are device pointers, 16-byte aligned (scales 4).  Up to 60 tensors share a
- * launch.  step counts from 1; the call holds it, lr and the betas by value, so a captured
- * graph repeats them.
+ * One launch, however many tensors: it reads them from a table in device memory.
+ * fp8_adamw_table writes that table (fp8_adamw_table_bytes bytes) into HOST memory, from an
+ * array in host memory of count descriptors whose pointers are device pointers, 16-byte
+ * aligned (scales 4), and the launch's size into *blocks; the caller copies the table to
+ * the device once (16-byte aligned) and keeps it for as long as the tensors stay where they are.
+ * fp8_adamw_step takes the device's copy, and the blocks and flags it was made with.
+ * step counts from 1; the call holds it, lr and the betas by value, so a captured graph
+ * repeats them.
  */
 typedef struct fp8_adamw_tensor {
     void* param;
@@ -541,8 +545,11 @@ typedef struct fp8_adamw_tensor {
     float* scale_v;
     int64_t n;
 } fp8_adamw_tensor;
-int fp8_adamw_step(const fp8_adamw_tensor* tensors, int64_t count, int flags, double lr, double beta1, double beta2,
-                   double eps, double weight_decay, int64_t step, const float* grad_scale, void* stream);
+size_t fp8_adamw_table_bytes(const fp8_adamw_tensor* tensors, int64_t count, int flags);
+int fp8_adamw_table(const fp8_adamw_tensor* tensors, int64_t count, int flags, void* table, size_t table_bytes,
+                    int64_t* blocks);
+int fp8_adamw_step(const void* table, int64_t blocks, int flags, double lr, double beta1, double beta2, double eps,
+                   double weight_decay, int64_t step, const float* grad_scale, void* stream);
 
 #ifdef __cplusplus
 }

@@ -10,25 +10,22 @@
 // zero is never stored as zero (it would leave m / eps): it becomes the smallest code.  The update of this step uses m and v from before
 // the rounding.
 //
-// The tensors of a launch lie in its arguments (up to 64 of them, no table in memory); a workgroup takes a piece of one of them.
+// One launch, however many tensors: the caller keeps a table of them in device memory, which also says for each workgroup which piece
+// of which tensor it has (a search through the sizes would be a chain of loads).  Pieces are 2048 elements, one trip of a
+// workgroup, or where that makes more workgroups than PLENTY, 8192.
 // Bound: HBM, 10 bytes an element (bfloat16, 8-bit moments) to 28 (all binary32).
 #include "fp8_device.hpp"
 #include "moe_launchers.hpp"
+
+#include <cstring>
 
 namespace fp8k {
 
 namespace {
 
 constexpr int NT = 256;
-constexpr int PIECE = 8192;       // elements of a workgroup
-constexpr int MOST = 60;          // tensors of a launch: the arguments hold 4 KB
-
-struct Many {
-    AdamwTensor t[MOST];
-    int first[MOST + 1];          // its first workgroup
-    int count;
-};
-static_assert(sizeof(Many) + sizeof(AdamwScalars) <= 4096, "kernel arguments");
+constexpr int TRIP = NT * 8;          // elements of a workgroup at a time
+constexpr int64_t PLENTY = 16384;     // workgroups
 
 struct Update {
     AdamwScalars s;
@@ -139,20 +136,19 @@ __device__ __forceinline__ float inverse_pow2(float s) { return __uint_as_float(
 
 // a thread: eight elements at a time; 32 lanes hold a block of 256
 template <class P, class G, bool FP8>
-__global__ __launch_bounds__(NT) void adamw_kernel(Many many, AdamwScalars s) {
-    int lo = 0, hi = many.count;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (many.first[mid] <= (int)blockIdx.x) lo = mid;
-        else hi = mid;
-    }
-    const AdamwTensor t = many.t[lo];
-    const int64_t i0 = (int64_t)((int)blockIdx.x - many.first[lo]) * PIECE;
+__global__ __launch_bounds__(NT) void adamw_kernel(const AdamwHeader* __restrict__ table, int flags, AdamwScalars s) {
+    const AdamwTensor* tensors = reinterpret_cast<const AdamwTensor*>(table + 1);
+    const int64_t count = table->count;
+    // (a table made for other types, or for fewer workgroups, changes nothing)
+    if (table->flags != flags || (int64_t)blockIdx.x >= table->blocks) return;
+    const AdamwBlock b = reinterpret_cast<const AdamwBlock*>(tensors + count)[blockIdx.x];
+    const AdamwTensor t = tensors[b.tensor];
+    const int rounds = table->rounds;
+    const int64_t i0 = (int64_t)b.piece * rounds * TRIP;
     const Update u{s, s.grad_scale ? *s.grad_scale : 1.0f};
     P* p = static_cast<P*>(t.p);
     const G* g = static_cast<const G*>(t.g);
-#pragma unroll 2
-    for (int r = 0; r < PIECE / (NT * 8); ++r) {
+    for (int r = 0; r < rounds; ++r) {
         const int64_t i = i0 + (int64_t)(r * NT + (int)threadIdx.x) * 8;
         const int64_t left = t.n - i;
         const int n = left >= 8 ? 8 : left > 0 ? (int)left : 0;
@@ -202,52 +198,47 @@ __global__ __launch_bounds__(NT) void adamw_kernel(Many many, AdamwScalars s) {
 }
 
 template <class P, class G>
-hipError_t launch_t(const Many& many, const AdamwScalars& s, bool fp8_state, hipStream_t st) {
-    const unsigned grid = (unsigned)many.first[many.count];
-    if (fp8_state) adamw_kernel<P, G, true><<<grid, NT, 0, st>>>(many, s);
-    else adamw_kernel<P, G, false><<<grid, NT, 0, st>>>(many, s);
+hipError_t launch_t(const void* table, int64_t blocks, int flags, const AdamwScalars& s, bool fp8_state, hipStream_t st) {
+    auto* h = static_cast<const AdamwHeader*>(table);
+    if (fp8_state) adamw_kernel<P, G, true><<<(unsigned)blocks, NT, 0, st>>>(h, flags, s);
+    else adamw_kernel<P, G, false><<<(unsigned)blocks, NT, 0, st>>>(h, flags, s);
     return hipGetLastError();
 }
 
+int64_t pieces(int64_t n, int rounds) { return (n + (int64_t)rounds * TRIP - 1) / ((int64_t)rounds * TRIP); }
+
 }  // namespace
 
-hipError_t launch_adamw(const AdamwTensor* tensors, int64_t count, bool p_f32, bool g_f32, bool fp8_state, const AdamwScalars& s, hipStream_t st) {
-    Many many;
-    many.count = 0;
-    many.first[0] = 0;
-    auto flush = [&]() -> hipError_t {
-        if (many.count == 0) return hipSuccess;
-        const hipError_t e = p_f32 ? (g_f32 ? launch_t<float, float>(many, s, fp8_state, st) : launch_t<float, __bf16>(many, s, fp8_state, st))
-                                   : (g_f32 ? launch_t<__bf16, float>(many, s, fp8_state, st) : launch_t<__bf16, __bf16>(many, s, fp8_state, st));
-        many.count = 0;
-        return e;
-    };
-    for (int64_t i = 0; i < count; ++i) {
-        AdamwTensor t = tensors[i];
-        while (t.n > 0) {
-            const int64_t room = (1 << 23) - (int64_t)(many.count ? many.first[many.count] : 0);      // workgroups left in the launch (a grid's threads are counted in 32 bits)
-            const int64_t want = (t.n + PIECE - 1) / PIECE, take = want < room ? want : room;
-            AdamwTensor part = t;
-            if (take < want) part.n = take * PIECE;
-            many.t[many.count] = part;
-            many.first[many.count + 1] = many.first[many.count] + (int)take;
-            ++many.count;
-            if (many.count == MOST || take < want)
-                if (hipError_t e = flush(); e != hipSuccess) return e;
-            if (take < want) {
-                const int64_t d = take * PIECE;
-                t.p = static_cast<char*>(t.p) + d * (p_f32 ? 4 : 2);
-                t.g = static_cast<const char*>(t.g) + d * (g_f32 ? 4 : 2);
-                t.m = static_cast<char*>(t.m) + d * (fp8_state ? 1 : 4);
-                t.v = static_cast<char*>(t.v) + d * (fp8_state ? 1 : 4);
-                if (fp8_state) { t.sm += d / 256; t.sv += d / 256; }
-                t.n -= d;
-            } else {
-                t.n = 0;
-            }
+AdamwHeader adamw_header(const AdamwTensor* tensors, int64_t count, int flags) {
+    AdamwHeader h{count, 0, flags, 1, 0};
+    for (int64_t i = 0; i < count; ++i) h.blocks += pieces(tensors[i].n, 1);
+    if (h.blocks > PLENTY) {
+        h.rounds = 4;
+        h.blocks = 0;
+        for (int64_t i = 0; i < count; ++i) h.blocks += pieces(tensors[i].n, 4);
+    }
+    if (h.blocks > (1 << 24) - 1) h.blocks = -1;      // (a grid's threads are counted in 32 bits)
+    return h;
+}
+
+void adamw_fill_table(const AdamwTensor* tensors, const AdamwHeader& h, void* table) {
+    char* at = static_cast<char*>(table);
+    std::memcpy(at, &h, sizeof(h));
+    at += sizeof(h);
+    for (int64_t i = 0; i < h.count; ++i, at += sizeof(AdamwTensor)) std::memcpy(at, &tensors[i], sizeof(AdamwTensor));
+    for (int64_t i = 0; i < h.count; ++i) {
+        const int64_t n = pieces(tensors[i].n, h.rounds);
+        for (int64_t j = 0; j < n; ++j, at += sizeof(AdamwBlock)) {
+            const AdamwBlock b{(int32_t)i, (int32_t)j};
+            std::memcpy(at, &b, sizeof(b));
         }
     }
-    return flush();
+}
+
+hipError_t launch_adamw(const void* table, int64_t blocks, int flags, bool p_f32, bool g_f32, bool fp8_state, const AdamwScalars& s, hipStream_t st) {
+    if (blocks <= 0) return hipSuccess;
+    if (p_f32) return g_f32 ? launch_t<float, float>(table, blocks, flags, s, fp8_state, st) : launch_t<float, __bf16>(table, blocks, flags, s, fp8_state, st);
+    return g_f32 ? launch_t<__bf16, float>(table, blocks, flags, s, fp8_state, st) : launch_t<__bf16, __bf16>(table, blocks, flags, s, fp8_state, st);
 }
 
 }  // namespace fp8k

@@ -303,6 +303,7 @@ hipError_t launch_t(const GroupedGemm& g, hipStream_t st) {
 template <int FA, int FB>
 hipError_t launch_rows(const GroupedGemm& g, hipStream_t st) {
     const int64_t mean = g.M / g.E;
+    if (mean >= 256 && gemm_fp8_grouped_stream_fits(g)) return launch_gemm_fp8_grouped_stream_rows(g, st);
     if (mean <= 16) return launch_t<FA, FB, 32, 128, 1, 4, 6, 1, false>(g, st);
     if (mean <= 64) return launch_t<FA, FB, 64, 128, 2, 2, 4, 8, false>(g, st);
     return launch_t<FA, FB, 128, 128, 2, 2, 4, 4, false>(g, st);
@@ -323,6 +324,7 @@ hipError_t launch_gemm_fp8_grouped_rows(const GroupedGemm& g, hipStream_t st) {
 
 template <int FA, int FB>
 static hipError_t launch_contract(const GroupedGemm& g, hipStream_t st) {
+    if (gemm_fp8_grouped_stream_fits(g)) return launch_gemm_fp8_grouped_stream_contract(g, st);
     return launch_t<FA, FB, 128, 128, 2, 2, 4, 4, true>(g, st);
 }
 hipError_t launch_gemm_fp8_grouped_contract(const GroupedGemm& g, hipStream_t st) { FP8K_FORMATS(launch_contract) }

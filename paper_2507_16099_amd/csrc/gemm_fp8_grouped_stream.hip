@@ -1,0 +1,470 @@
+// Large products grouped by expert: the persistent kernel of gemm_fp8_stream.hpp (one workgroup per CU walks many 256 x 256 tiles, the
+// epilogue of a tile drained inside the K steps of the next; its schedule, LDS layout and wait counts are described there) over the
+// tiles of all groups.
+//
+// What is different: the tiles.  A workgroup first reads the offsets and leaves in LDS, behind the stages, where each group's rows
+// start and how many tiles the groups before it have; the tile list is then walked like that of one product.
+//   rows      a tile's rows end with its group; the rows behind the last group are tiles without codes, which come out as zeros
+//   contract  the length of the contraction is the group's: at least four K steps are walked, those past its end fetch zeros
+// (A lookup is a few LDS reads per tile, between two K steps.)
+// Tiles are dealt in rounds: the eight XCDs work on neighbouring runs of the tile order at any time, so that every round has tiles of
+// about the same group and all workgroups contract about the same length.  An XCD's own contiguous range of all tiles, as in the
+// ungrouped kernel, gives it a group or two, and the largest group decides (dW of eight experts 14336 x 4096, 16384 skewed rows:
+// 1287 -> 807 us; rows of the same 799 -> 769 and 757 -> 700).
+// Measured: that dW 2380 TFLOP/s, the forward 2500, dX 2750; one 128 x 128 tile per workgroup 860, 1420, 1580.
+#include "gemm_fp8_stream.hpp"
+#include "group_tiles.hpp"
+#include "moe_launchers.hpp"
+
+namespace fp8k {
+
+namespace {
+
+constexpr int TABLE_GROUPS = (160 * 1024 - st::LDS_BYTES) / 12 - 2;      // what the LDS has left holds three numbers per group
+
+struct GroupedStreamArgs {
+    const uint8_t* A; int64_t lda; const uint8_t* B; int64_t ldb;
+    const float *scale_a, *scale_b;
+    const int32_t* offsets;
+    int E, M, N, K;              // rows: out [M, N] over K.  contract: out [E][N][K] over the group's rows
+    uint16_t* out; int64_t ld_out;
+    int tiles_m, tiles_n;        // tiles_m: of one group's output (contract)
+};
+
+// operand panels of one tile, and where its result goes
+struct GroupedTile {
+    v4i_t2 rsrc_a, rsrc_b;
+    int row, rows;               // first row of the output (and of scale_a), rows that exist
+    int n0, brow;                // first column; first entry of scale_b
+    int k;                       // codes contracted
+    int valid;
+};
+
+template <int FA, int FB, int AF1, bool CONTRACT>
+__global__ __launch_bounds__(st::NT) void gemm_fp8_grouped_stream_kernel(GroupedStreamArgs p) {
+    using namespace st;
+    static_assert(AF1 >= 2 && AF1 <= 4, "the A1 group has two to four fragments");
+    constexpr int TM = 32 * (4 + AF1);     // tile height: 256, 224 or 192 rows (the LDS layout keeps room for 256)
+    constexpr int NLA = TM / 32;           // LDS-DMA loads of the A part per wave and K step
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+
+    const int64_t lda = p.lda, ldb = p.ldb, ld_out = p.ld_out;
+    const float *scale_a = p.scale_a, *scale_b = p.scale_b;
+    const int N = CONTRACT ? p.K : p.N;      // columns of the output
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm0 = (wave >> 1) * (TM / 2), wn0 = (wave & 1) * WN;
+
+    // ---- the groups: starts[e] the first row, tiles_to[e] tiles of the groups before e, pads[e] the group's place in the padded order
+    int* const starts = reinterpret_cast<int*>(smem + 2 * STAGE + 2 * TAB);
+    int *const tiles_to = starts + p.E + 2, *const pads = tiles_to + p.E + 2;
+    if (wave == 0) {
+        int end = 0, tiles_before = 0, pad_before = 0;
+        for (int e0 = 0; e0 <= p.E; e0 += 64) {
+            const int e = e0 + lane;
+            int g_end = e < p.E ? p.offsets[e + 1] : e == p.E ? p.M : 0;
+            g_end = g_end < end ? end : g_end > p.M ? p.M : g_end;
+            g_end = wave_scan_max(g_end);
+            int g_start = __shfl_up(g_end, 1, 64);
+            if (lane == 0) g_start = end;
+            const int tiles = (g_end - g_start + TM - 1) / TM, pad = (g_end - g_start + 127) & ~127;
+            const int tiles_sum = tiles_before + wave_scan_add(tiles), pad_sum = pad_before + wave_scan_add(pad);
+            if (e <= p.E) {
+                starts[e] = g_start;
+                tiles_to[e] = tiles_sum - tiles;
+                pads[e] = pad_sum - pad;
+            }
+            if (e == p.E) {
+                starts[e + 1] = g_end;
+                tiles_to[e + 1] = tiles_sum;
+            }
+            end = __shfl(g_end, 63, 64);
+            tiles_before = __shfl(tiles_sum, 63, 64);
+            pad_before = __shfl(pad_sum, 63, 64);
+        }
+    }
+    __syncthreads();
+
+    // ---- this workgroup's tiles
+    const int tiles_n = p.tiles_n, per_group = p.tiles_m * tiles_n;
+    const int row_tiles = CONTRACT ? p.tiles_m * p.E : __builtin_amdgcn_readfirstlane(tiles_to[p.E + 1]);
+    const int units = row_tiles * tiles_n;
+    const int slots = gridDim.x / NUM_XCD;
+    const int xcd = blockIdx.x % NUM_XCD, slot = blockIdx.x / NUM_XCD;
+    const int u_first = xcd * slots + slot, u_step = NUM_XCD * slots;
+    if (u_first >= units) return;
+    const int my_tiles = (units - u_first + u_step - 1) / u_step;
+
+    auto tile_of = [&](int j) {
+        GroupedTile t;
+        t.valid = (j < my_tiles) ? 1 : 0;
+        const int logical = t.valid ? u_first + j * u_step : u_first;      // a missing tile aliases a valid one (its loads are forced out of range)
+        const int e_c = CONTRACT ? logical / per_group : 0;
+        const int rest = logical - e_c * per_group, in_group = GROUP_M * tiles_n, most_m = CONTRACT ? p.tiles_m : row_tiles;
+        const int first_m = (rest / in_group) * GROUP_M;
+        const int gsize = most_m - first_m < GROUP_M ? most_m - first_m : GROUP_M;
+        const int tm = first_m + (rest % in_group) % gsize;
+        t.n0 = (rest % in_group) / gsize * BN;
+        const int cols = N - t.n0 < BN ? N - t.n0 : BN;
+        uint64_t pa, pb;
+        if constexpr (CONTRACT) {
+            const int start = __builtin_amdgcn_readfirstlane(starts[e_c]), pad0 = __builtin_amdgcn_readfirstlane(pads[e_c]);
+            t.k = (__builtin_amdgcn_readfirstlane(starts[e_c + 1]) - start + 15) & ~15;
+            const int m0 = tm * TM;
+            t.row = e_c * p.N + m0;
+            t.rows = p.N - m0 < TM ? p.N - m0 : TM;
+            t.brow = e_c * p.K + t.n0;
+            pa = reinterpret_cast<uint64_t>(p.A + (int64_t)m0 * lda + pad0);
+            pb = reinterpret_cast<uint64_t>(p.B + (int64_t)t.n0 * ldb + pad0);
+        } else {
+            int e = 0;      // groups that end at or before tile tm
+            for (int e0 = 0; e0 <= p.E; e0 += 64) {
+                const int l = e0 + (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));      // (no register kept for the lane)
+                e += __popcll(__ballot(l <= p.E && tiles_to[l <= p.E ? l + 1 : 0] <= tm));
+            }
+            e = __builtin_amdgcn_readfirstlane(e);
+            t.row = __builtin_amdgcn_readfirstlane(starts[e]) + (tm - __builtin_amdgcn_readfirstlane(tiles_to[e])) * TM;
+            t.rows = __builtin_amdgcn_readfirstlane(starts[e + 1]) - t.row;
+            if (t.rows > TM) t.rows = TM;
+            t.k = e < p.E ? p.K : 0;
+            t.brow = (e < p.E ? e : p.E - 1) * p.N + t.n0;
+            pa = reinterpret_cast<uint64_t>(p.A + (int64_t)t.row * lda);
+            pb = reinterpret_cast<uint64_t>(p.B + (int64_t)t.brow * ldb);
+        }
+        t.rsrc_a = v4i_t2{(int)(uint32_t)pa, (int)(uint32_t)(pa >> 32), (int)((int64_t)(t.rows - 1) * lda + t.k), 0x00020000};
+        t.rsrc_b = v4i_t2{(int)(uint32_t)pb, (int)(uint32_t)(pb >> 32), (int)((int64_t)(cols - 1) * ldb + t.k), 0x00020000};
+        return t;
+    };
+
+    // ---- global -> LDS (as in the non-persistent kernel): wave w fills row groups w, w+4, ... (8 rows each) of both
+    //      tiles; lane l fills (row l/8, chunk slot l%8) with logical chunk slot ^ key(row).  The A part has TM rows:
+    //      NLA loads per wave (rows past TM are never read: the wave halves start at TM / 2).
+    const int lrow = lane >> 3;
+    const int ca = (lane & 7) ^ ((4 * (wave & 1) + (lrow >> 1)) & 7);
+    const int cb_e = (lane & 7) ^ (((lrow >> 1) & 1) | (((wave >> 1) & 3) << 1));
+    const int cb_o = (lane & 7) ^ (((lrow >> 1) & 1) | (((2 + (wave >> 1)) & 3) << 1));
+    const uint32_t va0 = (uint32_t)((wave * 8 + lrow) * (int)lda + ca * 16);
+    const uint32_t vb0_e = (uint32_t)((wave * 8 + lrow) * (int)ldb + cb_e * 16);
+    const uint32_t vb0_o = (uint32_t)((wave * 8 + lrow) * (int)ldb + cb_o * 16);
+    const uint32_t va_step = (uint32_t)(32 * (int)lda), vb_step = (uint32_t)(32 * (int)ldb);
+    const uint32_t lds_base = (uint32_t)(size_t)smem + (uint32_t)wave * 1024u;
+    constexpr uint32_t OOB = 0x80000000u;   // no valid offset reaches 2^31: adding it puts a lane outside its descriptor
+
+    // byte offsets of a K position in the three lane classes, forced out of range past K or for a missing tile
+    struct KOff { uint32_t a, e, o; };
+    auto koff = [&](int k0, const GroupedTile& t) {
+        KOff r;
+        r.a = (t.valid && k0 + ca * 16 < t.k) ? (uint32_t)k0 : OOB;
+        r.e = (t.valid && k0 + cb_e * 16 < t.k) ? (uint32_t)k0 : OOB;
+        r.o = (t.valid && k0 + cb_o * 16 < t.k) ? (uint32_t)k0 : OOB;
+        return r;
+    };
+    auto issue_loads = [&](const GroupedTile& t, int stage, int k0) {
+        const KOff ko = koff(k0, t);
+        const uint32_t la = lds_base + (uint32_t)(stage * STAGE), lb = la + BM * BK;
+#pragma unroll
+        for (int i = 0; i < NLA; ++i) st_lds_dma16(t.rsrc_a, la + i * 4096, va0 + (uint32_t)i * va_step + ko.a);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            st_lds_dma16(t.rsrc_b, lb + i * 4096, ((i & 1) ? vb0_o + ko.o : vb0_e + ko.e) + (uint32_t)i * vb_step);
+    };
+
+    // ---- LDS -> fragments
+    const int r16 = lane & 15, g = lane >> 4;
+    const int key_a = (r16 >> 1) & 7;
+    const int key_b = ((r16 >> 1) & 1) | ((r16 >> 2) << 1);
+    int offa[2], offb[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        offa[c] = (wm0 + r16) * BK + (((g + 4 * c) ^ key_a) << 4);
+        offb[c] = BM * BK + (wn0 + 16 * (r16 >> 2) + (r16 & 3)) * BK + (((g + 4 * c) ^ key_b) << 4);
+    }
+    v8i_t2 af[2][4], bf[2][4];   // [half][fragment in half]
+    auto read_a = [&](const uint8_t* s, int half, int f) {
+        const int row_off = (half * 4 + f) * 16 * BK;
+        const uint4 x0 = *reinterpret_cast<const uint4*>(s + offa[0] + row_off);
+        const uint4 x1 = *reinterpret_cast<const uint4*>(s + offa[1] + row_off);
+        af[half][f] = v8i_t2{(int)x0.x, (int)x0.y, (int)x0.z, (int)x0.w, (int)x1.x, (int)x1.y, (int)x1.z, (int)x1.w};
+    };
+    auto read_b = [&](const uint8_t* s, int half, int f) {
+        const int row_off = (half * 64 + f * 4) * BK;
+        const uint4 x0 = *reinterpret_cast<const uint4*>(s + offb[0] + row_off);
+        const uint4 x1 = *reinterpret_cast<const uint4*>(s + offb[1] + row_off);
+        bf[half][f] = v8i_t2{(int)x0.x, (int)x0.y, (int)x0.z, (int)x0.w, (int)x1.x, (int)x1.y, (int)x1.z, (int)x1.w};
+    };
+
+    v4f_t2 acc[8][8];   // [A fragment][B fragment]
+
+    // ---- drain.  Lane (g, r16) holds, per A fragment fi, output row 16 fi + r16 of the wave's quadrant and, per B
+    //      half, the 16 consecutive columns 64 BH + 16 g + x, x = 4 t + r (B fragment t, accumulator register r).
+    //      The output of a tile is addressed through a raw buffer that starts at the tile's first element and ends
+    //      with the last valid output row: rows past M are dropped by the bounds check.
+    struct Drain {
+        __amdgpu_buffer_rsrc_t rsrc;   // output window of the tile
+        const float* tab;   // reciprocal scales of that tile: [0,256) rows, [256,512) columns
+        int n_left;         // N - n0: columns of the tile that exist
+    };
+    const uint32_t lane_out = (uint32_t)(((wm0 + r16) * (int)ld_out + wn0 + 8 * g) * 2);   // byte offset of this lane's first piece in a tile
+    const int lane_col = wn0 + 8 * g;
+    float inv_b[4][4], inv_a = 0.f;     // the job's sixteen column scales and its row scale
+    uint32_t pk[8];
+    // step S of a job: 0 = fetch its row scale and first column scales; 1..4 = read four accumulators (one B fragment),
+    // scale, round, pack, and fetch the next fragment's column scales; 5 = regroup and store
+    auto job_step = [&](auto job_t, auto step_t, const Drain& d) {
+        using J = decltype(job_t);
+        constexpr int S = decltype(step_t)::value;
+        if constexpr (!J::none(AF1)) {
+            constexpr int AH = J::AH, BH = J::BH, U = J::U;
+            if constexpr (S == 0) {
+                // all of the job's scales in one go (one wait for LDS per job instead of five; measured neutral)
+                inv_a = d.tab[wm0 + 16 * (AH * 4 + U) + r16];
+#pragma unroll
+                for (int T = 0; T < 4; ++T) {
+                    const float4 t4 = *reinterpret_cast<const float4*>(d.tab + 256 + wn0 + 64 * BH + 16 * g + 4 * T);
+                    inv_b[T][0] = t4.x; inv_b[T][1] = t4.y; inv_b[T][2] = t4.z; inv_b[T][3] = t4.w;
+                }
+            } else if constexpr (S <= 4) {
+                constexpr int T = S - 1;                                   // B fragment of the half
+                const v4f_t2 v = acc[AH * 4 + U][BH * 4 + T];
+                pk[2 * T] = st_pack_bf16((v[0] * inv_a) * inv_b[T][0], (v[1] * inv_a) * inv_b[T][1]);
+                pk[2 * T + 1] = st_pack_bf16((v[2] * inv_a) * inv_b[T][2], (v[3] * inv_a) * inv_b[T][3]);
+            } else {
+                // lanes g = 0..3 of a row hold the 16-byte pieces (2g, 2g+1) of its 128 bytes; after the two swaps
+                // lane g holds pieces g (lo) and 4 + g (hi): each store writes 64 contiguous bytes per row
+                uint32_t lo[4], hi[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const v2u_t2 s1 = __builtin_amdgcn_permlane16_swap(pk[e], pk[4 + e], false, false);
+                    const v2u_t2 s2 = __builtin_amdgcn_permlane32_swap(s1[0], s1[1], false, false);
+                    lo[e] = s2[0]; hi[e] = s2[1];
+                }
+                // (offsets formed here, from values the optimizer cannot see through: hoisted out of the tile loop,
+                //  the sixteen jobs' offsets would be sixteen more live registers)
+                uint32_t lo_base = lane_out;
+                int ld32 = (int)ld_out;
+                asm volatile("" : "+v"(lo_base), "+s"(ld32));
+                const uint32_t off = lo_base + (uint32_t)((16 * (AH * 4 + U) * ld32 + 64 * BH) * 2);
+                const uint32_t off_lo = lane_col + 64 * BH < d.n_left ? off : OOB;
+                const uint32_t off_hi = lane_col + 64 * BH + 32 < d.n_left ? off + 64u : OOB;
+                __builtin_amdgcn_raw_buffer_store_b128(v4u_t2{lo[0], lo[1], lo[2], lo[3]}, d.rsrc, (int)off_lo, 0, 2);   // 2: non-temporal
+                __builtin_amdgcn_raw_buffer_store_b128(v4u_t2{hi[0], hi[1], hi[2], hi[3]}, d.rsrc, (int)off_hi, 0, 2);
+            }
+        }
+    };
+    // slot t of a phase carrying the jobs JS
+    auto jobs_slot = [&](auto jobs_t, auto slot_t, const Drain& d) {
+        using JS = decltype(jobs_t);
+        constexpr int T = decltype(slot_t)::value;
+        if constexpr (T <= 5) job_step(typename JS::J0{}, std::integral_constant<int, T>{}, d);
+        if constexpr (T >= 5 && T <= 10) job_step(typename JS::J1{}, std::integral_constant<int, T - 5>{}, d);
+        if constexpr (T >= 10) job_step(typename JS::J2{}, std::integral_constant<int, T - 10>{}, d);
+    };
+
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, 1>;
+    using I5 = std::integral_constant<int, 5>;
+    using I6 = std::integral_constant<int, 6>;
+    using I11 = std::integral_constant<int, 11>;
+
+    // one phase: 16 MFMAs of A half AH x B half BH (ZERO: starting from C = 0); in its slots, optionally the reads of
+    // one fragment half (RDA: 1 = A half RH, 0 = B half RH) from stage `rs`, CNT of the step's sixteen LDS-DMA refill
+    // loads from number L0 on (0-7: the B part, 8-15: the A part) out of tile `lt` at K offsets `ko`, and the drain
+    // jobs JS of the tile described by `dr`.  Order inside a slot: MFMA, fragment reads, refill load, drain work.
+    auto phase = [&](auto ah_t, auto bh_t, auto rda_t, auto rh_t, auto l0_t, auto cnt_t, auto zero_t, auto jobs_t, const uint8_t* rs,
+                     uint32_t la, uint32_t lb, const GroupedTile& lt, const KOff& ko, const Drain& dr) {
+        constexpr int AH = decltype(ah_t)::value, BH = decltype(bh_t)::value, RDA = decltype(rda_t)::value,
+                      RH = decltype(rh_t)::value, L0 = decltype(l0_t)::value, CNT = decltype(cnt_t)::value,
+                      ZERO = decltype(zero_t)::value;
+        using JS = decltype(jobs_t);
+        constexpr bool DRAINS = JS::stores(AF1) > 0;
+        [&]<int... TS>(std::integer_sequence<int, TS...>) {
+            ([&] {
+                constexpr int t = TS;
+                constexpr int i = t >> 2, j = (i & 1) ? 3 - (t & 3) : (t & 3);   // boustrophedon: one operand stays between neighbours
+                if constexpr (AH == 0 || i < AF1) {        // (a lower tile has no fragment i of the A1 group: the slot stays empty)
+                    if constexpr (ZERO) st_mfma_zero<FA, FB>(acc[AH * 4 + i][BH * 4 + j], bf[BH][j], af[AH][i]);
+                    else st_mfma<FA, FB>(acc[AH * 4 + i][BH * 4 + j], bf[BH][j], af[AH][i]);
+                }
+                if constexpr (RDA == 1 && t % 2 == 0 && t < 8 && (RH == 0 || t / 2 < AF1)) read_a(rs, RH, t / 2);
+                if constexpr (RDA == 0 && t % 2 == 0 && t < 8) read_b(rs, RH, t / 2);
+                if constexpr (t % 2 == 1 && t / 2 < CNT) {
+                    constexpr int q = L0 + t / 2;
+                    if constexpr (q < 8) st_lds_dma16(lt.rsrc_b, lb + q * 4096, ((q & 1) ? vb0_o + ko.o : vb0_e + ko.e) + (uint32_t)q * vb_step);
+                    else if constexpr (q - 8 < NLA) st_lds_dma16(lt.rsrc_a, la + (q - 8) * 4096, va0 + (uint32_t)(q - 8) * va_step + ko.a);
+                }
+                if constexpr (DRAINS) {
+                    __builtin_amdgcn_sched_barrier(0);     // the slot's refill load is issued before its stores (the wait counts rely on it)
+                    jobs_slot(JS{}, std::integral_constant<int, t>{}, dr);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }(), ...);
+        }(std::make_integer_sequence<int, 16>{});
+    };
+
+    // pairs of K steps of a tile: two at least, an odd count of steps gets one of zeros
+    auto kpairs_of = [&](const GroupedTile& t) {
+        const int pairs = ((t.k + BK - 1) / BK + 1) / 2;
+        return pairs < 2 ? 2 : pairs;
+    };
+
+    // reciprocal scales of a tile, one row and one column per thread (correctly rounded divides).  The raw scales come into
+    // the table by LDS-DMA, each wave those of its own threads: the compiler, which sees no load, places no wait for them
+    // (it would also wait for the operands in flight), and no register stands for a load that has not arrived.
+    auto scale_loads = [&](const GroupedTile& t, float* tab) {
+        const int cols = N - t.n0 < BN ? N - t.n0 : BN, i = (int)threadIdx.x;
+        const uint64_t pa = reinterpret_cast<uint64_t>(scale_a + t.row), pb = reinterpret_cast<uint64_t>(scale_b + t.brow);
+        const v4i_t2 rsrc_a = {(int)(uint32_t)pa, (int)(uint32_t)(pa >> 32), t.rows * 4, 0x00020000};
+        const v4i_t2 rsrc_b = {(int)(uint32_t)pb, (int)(uint32_t)(pb >> 32), cols * 4, 0x00020000};
+        const uint32_t at = (uint32_t)(size_t)tab + (uint32_t)wave * 256u;
+        st_lds_dma4(rsrc_a, at, (uint32_t)(i < t.rows ? i : t.rows - 1) * 4u);
+        st_lds_dma4(rsrc_b, at + 1024u, (uint32_t)(i < cols ? i : cols - 1) * 4u);
+    };
+    auto scale_table = [&](const GroupedTile& t, float* tab) {
+        // (the loads were issued ahead of a phase 3's refill loads and a wait that lets only younger operations stay in flight has
+        // passed; a tile without codes is zero whatever stands in its rows' scales)
+        const float raw_a = tab[threadIdx.x], raw_b = tab[256 + threadIdx.x];
+        tab[threadIdx.x] = t.k ? 1.0f / raw_a : 0.0f;
+        tab[256 + threadIdx.x] = 1.0f / raw_b;
+    };
+    float* const tab0 = reinterpret_cast<float*>(smem + 2 * STAGE);
+
+    auto drain_of = [&](const GroupedTile& t, int j) {
+        Drain d;
+        d.n_left = N - t.n0;
+        const int cols = d.n_left < BN ? d.n_left : BN;
+        d.rsrc = __builtin_amdgcn_make_buffer_rsrc(p.out + (int64_t)t.row * ld_out + t.n0, 0, (int)(((int64_t)(t.rows - 1) * ld_out + cols) * 2), 0x00020000);
+        d.tab = tab0 + (j & 1) * (TAB / 4);
+        return d;
+    };
+
+    // a pair of K steps (the B halves swap roles every step).  KIND: ST_FIRST(_DRAIN) = steps 0, 1 of a tile (step 0
+    // starts the accumulators from zero; with _DRAIN the rest of the previous tile leaves in its phases 1-3; the scale
+    // loads of this tile go out in step 0, its table is written in step 1), ST_MIDDLE, ST_LAST = the last two steps
+    // (refills fetch steps 0, 1 of tile `lt` = the next tile; the drain of this tile starts in phase 2 of the last step).
+    auto pair = [&](auto kind_t, const GroupedTile& cur, const GroupedTile& lt, int k2_even, const Drain& dprev, const Drain& dcur, float* tab_cur) {
+        constexpr int KIND = decltype(kind_t)::value;
+        constexpr bool FIRST = KIND == ST_FIRST || KIND == ST_FIRST_DRAIN;
+        constexpr bool FD = KIND == ST_FIRST_DRAIN, LD = KIND == ST_LAST;
+        using Z = std::integral_constant<int, FIRST ? 1 : 0>;
+        using NJ = StNoJobs;
+        {
+            // even step: B order 0,1,1,0.  Holds A0, B0 of this step.
+            const uint8_t* s_cur = smem;
+            const uint8_t* s_nxt = smem + STAGE;
+            const KOff ko = koff(k2_even, lt);
+            const uint32_t la = lds_base, lb = la + BM * BK;
+            phase(I0{}, I0{}, I0{}, I1{}, I0{}, I0{}, Z{}, std::conditional_t<FD, StJobsF1, NJ>{}, s_cur, la, lb, lt, ko, dprev);   // (A0,B0) | read B1 of this step
+            st_barrier_lds();                  // this step's B part is read out by everyone
+            phase(I0{}, I1{}, I1{}, I1{}, I0{}, I5{}, Z{}, std::conditional_t<FD, StJobsF2, NJ>{}, s_cur, la, lb, lt, ko, dprev);   // (A0,B1) | read A1 of this step, refill B 0-4
+            st_wait_vmem_but_barrier<5 + (FD ? st_extra_f(AF1) : 0)>();   // step k+1 has landed for everyone; this step's A part is read out
+            if constexpr (FIRST) scale_loads(cur, tab_cur);   // older than the refill loads below: complete at the next such wait
+            phase(I1{}, I1{}, I1{}, I0{}, I5{}, I6{}, Z{}, std::conditional_t<FD, StJobsF3, NJ>{}, s_nxt, la, lb, lt, ko, dprev);   // (A1,B1) | read A0 of step k+1, refill B 5-7, A 0-2
+            phase(I1{}, I0{}, I0{}, I1{}, I11{}, I5{}, Z{}, NJ{}, s_nxt, la, lb, lt, ko, dprev);                                    // (A1,B0) | read B1 of step k+1, refill A 3-7
+        }
+        {
+            // odd step: B order 1,0,0,1.  Holds A0, B1 of this step.
+            const uint8_t* s_cur = smem + STAGE;
+            const uint8_t* s_nxt = smem;
+            const KOff ko = koff(k2_even + BK, lt);
+            const uint32_t la = lds_base + (uint32_t)STAGE, lb = la + BM * BK;
+            phase(I0{}, I1{}, I0{}, I0{}, I0{}, I0{}, I0{}, NJ{}, s_cur, la, lb, lt, ko, dcur);                                     // (A0,B1) | read B0 of this step
+            st_barrier_lds();
+            phase(I0{}, I0{}, I1{}, I1{}, I0{}, I5{}, I0{}, std::conditional_t<LD, StJobsL2, NJ>{}, s_cur, la, lb, lt, ko, dcur);   // (A0,B0) | read A1 of this step, refill B 0-4
+            st_wait_vmem_but_barrier<5 + (LD ? st_extra_l(AF1) : 0)>();
+            if constexpr (FIRST) scale_table(cur, tab_cur);
+            phase(I1{}, I0{}, I1{}, I0{}, I5{}, I6{}, I0{}, std::conditional_t<LD, StJobsL3, NJ>{}, s_nxt, la, lb, lt, ko, dcur);   // (A1,B0) | read A0 of step k+1, refill B 5-7, A 0-2
+            phase(I1{}, I1{}, I0{}, I0{}, I11{}, I5{}, I0{}, std::conditional_t<LD, StJobsL4, NJ>{}, s_nxt, la, lb, lt, ko, dcur);  // (A1,B1) | read B0 of step k+1, refill A 3-7
+        }
+    };
+
+    // ---- first tile: both stages in flight at once, then the first fragments
+    GroupedTile cur = tile_of(0);
+    issue_loads(cur, 0, 0);
+    issue_loads(cur, 1, BK);
+    st_wait_all_vmem();
+    __syncthreads();
+#pragma unroll
+    for (int f = 0; f < 4; ++f) {
+        read_a(smem, 0, f);
+        read_b(smem, 0, f);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+
+    GroupedTile prev = cur;
+    for (int j = 0; j < my_tiles; ++j) {
+        float* tab_cur = tab0 + (j & 1) * (TAB / 4);
+        const int kpairs = kpairs_of(cur);
+        {
+            const Drain dprev = drain_of(prev, j - 1);
+            if (j == 0) pair(std::integral_constant<int, ST_FIRST>{}, cur, cur, 2 * BK, dprev, dprev, tab_cur);
+            else pair(std::integral_constant<int, ST_FIRST_DRAIN>{}, cur, cur, 2 * BK, dprev, dprev, tab_cur);
+        }
+        for (int kp = 1; kp < kpairs - 1; ++kp) {
+            const Drain none = drain_of(cur, j);
+            pair(std::integral_constant<int, ST_MIDDLE>{}, cur, cur, (2 * kp + 2) * BK, none, none, tab_cur);
+        }
+        const GroupedTile nxt = tile_of(j + 1);
+        {
+            const Drain dcur = drain_of(cur, j);
+            pair(std::integral_constant<int, ST_LAST>{}, cur, nxt, 0, dcur, dcur, tab_cur);
+        }
+        prev = cur;
+        cur = nxt;
+    }
+    st_wait_all_vmem();    // the trailing refills (all out of range) have landed
+
+    // ---- what is left of the last tile: the jobs that the next tile's first step would have carried
+    {
+        const Drain dlast = drain_of(prev, my_tiles - 1);
+        [&]<int... TS>(std::integer_sequence<int, TS...>) {
+            (jobs_slot(StJobsF1{}, std::integral_constant<int, TS>{}, dlast), ...);
+            (jobs_slot(StJobsF2{}, std::integral_constant<int, TS>{}, dlast), ...);
+            (jobs_slot(StJobsF3{}, std::integral_constant<int, TS>{}, dlast), ...);
+        }(std::make_integer_sequence<int, 16>{});
+    }
+}
+
+template <int FA, int FB, int AF1, bool CONTRACT>
+hipError_t launch_t(const GroupedGemm& g, hipStream_t st) {
+    using namespace st;
+    constexpr int TM = 32 * (4 + AF1);
+    auto kern = gemm_fp8_grouped_stream_kernel<FA, FB, AF1, CONTRACT>;
+    static DynamicLdsOnce attr;
+    if (hipError_t e = attr.ensure(reinterpret_cast<const void*>(kern), 160 * 1024); e != hipSuccess) return e;
+    int64_t cus = compute_units();
+    if (const int forced = knob(KNOB_GEMM_STREAM); forced >= NUM_XCD) cus = forced;
+    if (cus < NUM_XCD) cus = NUM_XCD;
+    const int64_t tiles_m = (g.N + TM - 1) / TM, tiles_n = ((CONTRACT ? g.K : g.N) + BN - 1) / BN;
+    const int64_t most = (CONTRACT ? tiles_m * g.E : g.M / TM + (g.E + 1 < g.M ? g.E + 1 : g.M)) * tiles_n;
+    if (most > 0x3FFFFFFF) return hipErrorNotSupported;
+    int64_t grid = cus / NUM_XCD * NUM_XCD;
+    if (const int64_t need = (most + NUM_XCD - 1) / NUM_XCD * NUM_XCD; grid > need) grid = need;
+    const GroupedStreamArgs a{g.a, g.lda, g.b, g.ldb, g.scale_a, g.scale_b, g.offsets, (int)g.E, (int)g.M, (int)g.N, (int)g.K,
+                              static_cast<uint16_t*>(g.out), g.ld_out, (int)tiles_m, (int)tiles_n};
+    kern<<<dim3((unsigned)grid), dim3(NT), LDS_BYTES + 12 * (int)(g.E + 2), st>>>(a);
+    return hipGetLastError();
+}
+
+template <int FA, int FB>
+hipError_t launch_rows(const GroupedGemm& g, hipStream_t st) { return launch_t<FA, FB, 4, false>(g, st); }
+template <int FA, int FB>
+hipError_t launch_contract(const GroupedGemm& g, hipStream_t st) {
+    const int64_t rows = gemm_fp8_stream_tile_m(g.N * g.E, g.K);
+    return rows == 256 ? launch_t<FA, FB, 4, true>(g, st) : rows == 224 ? launch_t<FA, FB, 3, true>(g, st) : launch_t<FA, FB, 2, true>(g, st);
+}
+
+}  // namespace
+
+bool gemm_fp8_grouped_stream_fits(const GroupedGemm& g) { return g.E <= TABLE_GROUPS && g.ld_out < (1 << 22); }
+
+#define FP8K_FORMATS(CALL)                                                                          \
+    if (g.fmt_a == FMT_E4M3FN && g.fmt_b == FMT_E4M3FN) return CALL<FMT_E4M3FN, FMT_E4M3FN>(g, st); \
+    if (g.fmt_a == FMT_E5M2 && g.fmt_b == FMT_E4M3FN) return CALL<FMT_E5M2, FMT_E4M3FN>(g, st);     \
+    if (g.fmt_a == FMT_E4M3FN) return CALL<FMT_E4M3FN, FMT_E5M2>(g, st);                            \
+    return CALL<FMT_E5M2, FMT_E5M2>(g, st);
+
+hipError_t launch_gemm_fp8_grouped_stream_rows(const GroupedGemm& g, hipStream_t st) { FP8K_FORMATS(launch_rows) }
+hipError_t launch_gemm_fp8_grouped_stream_contract(const GroupedGemm& g, hipStream_t st) { FP8K_FORMATS(launch_contract) }
+
+}  // namespace fp8k

@@ -336,21 +336,19 @@ int fp8_grouped_linear_fwd_prequantized(const void* x, int64_t T, const int32_t*
     return FP8_OK;
 }
 
-int fp8_adamw_step(const fp8_adamw_tensor* tensors, int64_t count, int flags, double lr, double beta1, double beta2, double eps,
-                   double weight_decay, int64_t step, const float* grad_scale, void* stream) {
-    const char* fn = "fp8_adamw_step";
-    api_error(FP8_OK, "");
-    if (flags & ~(FP8_ADAMW_PARAM_FP32 | FP8_ADAMW_GRAD_FP32 | FP8_ADAMW_STATE_FP8)) return fail(FP8_ERR_ENUM, "%s: flags=%d has unknown bits", fn, flags);
-    if (count < 0) return fail(FP8_ERR_SHAPE, "%s: count=%lld is negative", fn, (ll)count);
-    if (!(lr >= 0) || !(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1) || !(eps >= 0) || !(weight_decay >= 0) || step < 1)
-        return fail(FP8_ERR_SHAPE, "%s: lr=%g betas=(%g, %g) eps=%g weight_decay=%g step=%lld out of range", fn, lr, beta1, beta2, eps, weight_decay, (ll)step);
-    if (!aligned(grad_scale, 4)) return fail(FP8_ERR_ALIGN, "%s: grad_scale not 4-byte aligned", fn);
-    if (count == 0) return FP8_OK;
-    if (!tensors) return fail(FP8_ERR_NULL, "%s: tensors is NULL", fn);
+static_assert(sizeof(fp8_adamw_tensor) == sizeof(fp8k::AdamwTensor), "the same layout");
+static const fp8k::AdamwTensor* as_internal(const fp8_adamw_tensor* t) { return reinterpret_cast<const fp8k::AdamwTensor*>(t); }
+
+constexpr int kAdamwFlags = FP8_ADAMW_PARAM_FP32 | FP8_ADAMW_GRAD_FP32 | FP8_ADAMW_STATE_FP8;
+
+static int check_adamw_tensors(const char* fn, const fp8_adamw_tensor* tensors, int64_t count, int flags) {
+    if (flags & ~kAdamwFlags) return fail(FP8_ERR_ENUM, "%s: flags=%d has unknown bits", fn, flags);
+    if (count < 0 || count > kMaxDim) return fail(FP8_ERR_SHAPE, "%s: count=%lld out of range", fn, (ll)count);
+    if (count > 0 && !tensors) return fail(FP8_ERR_NULL, "%s: tensors is NULL", fn);
     const bool q = flags & FP8_ADAMW_STATE_FP8;
     for (int64_t i = 0; i < count; ++i) {
         const fp8_adamw_tensor& t = tensors[i];
-        if (t.n < 0) return fail(FP8_ERR_SHAPE, "%s: tensor %lld has n=%lld", fn, (ll)i, (ll)t.n);
+        if (t.n < 0 || t.n > (int64_t)1 << 37) return fail(FP8_ERR_SHAPE, "%s: tensor %lld has n=%lld", fn, (ll)i, (ll)t.n);
         if (t.n == 0) continue;
         if (!t.param || !t.grad || !t.exp_avg || !t.exp_avg_sq || (q && (!t.scale_m || !t.scale_v)))
             return fail(FP8_ERR_NULL, "%s: tensor %lld has a NULL pointer", fn, (ll)i);
@@ -358,12 +356,46 @@ int fp8_adamw_step(const fp8_adamw_tensor* tensors, int64_t count, int flags, do
             (q && (!aligned(t.scale_m, 4) || !aligned(t.scale_v, 4))))
             return fail(FP8_ERR_ALIGN, "%s: tensor %lld: a pointer is not 16-byte (scales: 4-byte) aligned", fn, (ll)i);
     }
-    static_assert(sizeof(fp8_adamw_tensor) == sizeof(fp8k::AdamwTensor), "the same layout");
+    if (fp8k::adamw_header(as_internal(tensors), count, flags).blocks < 0) return fail(FP8_ERR_SHAPE, "%s: too many elements for a launch", fn);
+    return FP8_OK;
+}
+
+size_t fp8_adamw_table_bytes(const fp8_adamw_tensor* tensors, int64_t count, int flags) {
+    api_error(FP8_OK, "");
+    if (check_adamw_tensors("fp8_adamw_table_bytes", tensors, count, flags)) return 0;
+    return fp8k::adamw_table_bytes(fp8k::adamw_header(as_internal(tensors), count, flags));
+}
+
+int fp8_adamw_table(const fp8_adamw_tensor* tensors, int64_t count, int flags, void* table, size_t table_bytes, int64_t* blocks) {
+    const char* fn = "fp8_adamw_table";
+    api_error(FP8_OK, "");
+    FP8_CHECK(check_adamw_tensors(fn, tensors, count, flags));
+    FP8_CHECK(need(fn, "table", table, 1));
+    FP8_CHECK(need(fn, "blocks", blocks, 8));
+    const fp8k::AdamwHeader h = fp8k::adamw_header(as_internal(tensors), count, flags);
+    const size_t want = fp8k::adamw_table_bytes(h);
+    if (table_bytes < want) return fail(FP8_ERR_WORKSPACE, "%s: table %zu < %zu bytes", fn, table_bytes, want);
+    fp8k::adamw_fill_table(as_internal(tensors), h, table);
+    *blocks = h.blocks;
+    return FP8_OK;
+}
+
+int fp8_adamw_step(const void* table, int64_t blocks, int flags, double lr, double beta1, double beta2, double eps, double weight_decay,
+                   int64_t step, const float* grad_scale, void* stream) {
+    const char* fn = "fp8_adamw_step";
+    api_error(FP8_OK, "");
+    if (flags & ~kAdamwFlags) return fail(FP8_ERR_ENUM, "%s: flags=%d has unknown bits", fn, flags);
+    if (blocks < 0 || blocks >= 1 << 24) return fail(FP8_ERR_SHAPE, "%s: blocks=%lld out of range", fn, (ll)blocks);
+    if (!(lr >= 0) || !(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1) || !(eps >= 0) || !(weight_decay >= 0) || step < 1)
+        return fail(FP8_ERR_SHAPE, "%s: lr=%g betas=(%g, %g) eps=%g weight_decay=%g step=%lld out of range", fn, lr, beta1, beta2, eps, weight_decay, (ll)step);
+    if (!aligned(grad_scale, 4)) return fail(FP8_ERR_ALIGN, "%s: grad_scale not 4-byte aligned", fn);
+    if (blocks == 0) return FP8_OK;
+    FP8_CHECK(need(fn, "table", table, 16));
     const double bc1 = 1.0 - std::pow(beta1, (double)step), bc2 = 1.0 - std::pow(beta2, (double)step);
     const fp8k::AdamwScalars s{(float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)(1.0 - lr * weight_decay),
                                (float)(lr / bc1), (float)(1.0 / std::sqrt(bc2)), (float)eps, grad_scale};
-    FP8_TRY(fp8k::launch_adamw(reinterpret_cast<const fp8k::AdamwTensor*>(tensors), count, flags & FP8_ADAMW_PARAM_FP32, flags & FP8_ADAMW_GRAD_FP32, q,
-                               s, static_cast<hipStream_t>(stream)));
+    FP8_TRY(fp8k::launch_adamw(table, blocks, flags, flags & FP8_ADAMW_PARAM_FP32, flags & FP8_ADAMW_GRAD_FP32, flags & FP8_ADAMW_STATE_FP8, s,
+                               static_cast<hipStream_t>(stream)));
     return FP8_OK;
 }
 

@@ -53,10 +53,20 @@ hipError_t launch_gemm_fp8_grouped_rows(const GroupedGemm& g, hipStream_t st);
 // out[e] [N, K] for each group: A [N, lda], B [K, ldb] with the group's columns where launch_quant_cols_grouped leaves them;
 // scale_a [E, N], scale_b [E, K]
 hipError_t launch_gemm_fp8_grouped_contract(const GroupedGemm& g, hipStream_t st);
+// the same on persistent workgroups with 256 x 256 tiles (gemm_fp8_grouped_stream.hip); _fits: the groups' table has room, 32-bit offsets reach
+bool gemm_fp8_grouped_stream_fits(const GroupedGemm& g);
+hipError_t launch_gemm_fp8_grouped_stream_rows(const GroupedGemm& g, hipStream_t st);
+hipError_t launch_gemm_fp8_grouped_stream_contract(const GroupedGemm& g, hipStream_t st);
 
 // ---- AdamW (adamw.hip)
 struct AdamwTensor { void* p; const void* g; void *m, *v; float *sm, *sv; int64_t n; };
 struct AdamwScalars { float b1, c1, b2, c2, decay, rate, inv_root, eps; const float* grad_scale; };
-hipError_t launch_adamw(const AdamwTensor* tensors, int64_t count, bool p_f32, bool g_f32, bool fp8_state, const AdamwScalars& s, hipStream_t st);
+// The table in device memory that a step reads: a header, the tensors, and for each workgroup which piece of which tensor it has.
+struct AdamwHeader { int64_t count, blocks; int32_t flags, rounds; int64_t reserved; };
+struct AdamwBlock { int32_t tensor, piece; };
+AdamwHeader adamw_header(const AdamwTensor* tensors, int64_t count, int flags);      // blocks < 0: too many
+inline size_t adamw_table_bytes(const AdamwHeader& h) { return sizeof(AdamwHeader) + (size_t)h.count * sizeof(AdamwTensor) + (size_t)h.blocks * sizeof(AdamwBlock); }
+void adamw_fill_table(const AdamwTensor* tensors, const AdamwHeader& h, void* table);
+hipError_t launch_adamw(const void* table, int64_t blocks, int flags, bool p_f32, bool g_f32, bool fp8_state, const AdamwScalars& s, hipStream_t st);
 
 }  // namespace fp8k

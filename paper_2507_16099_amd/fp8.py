@@ -185,6 +185,10 @@ def load_library() -> C.CDLL:
     L.fp8_grouped_linear_prequantized_workspace_bytes.argtypes = [i64, i64]
     L.fp8_grouped_linear_fwd_prequantized.restype = ci
     L.fp8_grouped_linear_fwd_prequantized.argtypes = [vp, i64, vp, ci, ci, vp, i64, ci, vp, vp, i64, i64, i64, i64, vp, vp, sz, vp]
+    L.fp8_adamw_table_bytes.restype = sz
+    L.fp8_adamw_table_bytes.argtypes = [vp, i64, ci]
+    L.fp8_adamw_table.restype = ci
+    L.fp8_adamw_table.argtypes = [vp, i64, ci, vp, sz, C.POINTER(i64)]
     L.fp8_adamw_step.restype = ci
     L.fp8_adamw_step.argtypes = [vp, i64, ci, C.c_double, C.c_double, C.c_double, C.c_double, C.c_double, i64, vp, vp]
     L.fp8_internal_set_knob.restype = ci
@@ -761,12 +765,13 @@ def fp8_moe_route(logits: torch.Tensor, k: int, flags: int = 0, out=None, worksp
     if workspace is None:
         workspace = torch.empty(fp8_moe_route_workspace_bytes(T, E, k), dtype=torch.uint8, device=dev)
     if out is None:
-        out = (torch.empty((T, k), dtype=torch.float32, device=dev), torch.empty((T, k), dtype=i32, device=dev),
-               torch.empty(E + 1, dtype=i32, device=dev), torch.empty(T * k, dtype=i32, device=dev),
-               torch.empty((T, k), dtype=i32, device=dev))
-    gates, experts, offsets, row_token, slot_row = out
-    _dense(gates, (T, k), torch.float32, "gates"), _dense(experts, (T, k), i32, "experts"), _dense(offsets, (E + 1,), i32, "offsets")
-    _dense(row_token, (T * k,), i32, "row_token"), _dense(slot_row, (T, k), i32, "slot_row")
+        gates, experts, offsets = torch.empty((T, k), dtype=torch.float32, device=dev), torch.empty((T, k), dtype=i32, device=dev), torch.empty(E + 1, dtype=i32, device=dev)
+        row_token, slot_row = torch.empty(T * k, dtype=i32, device=dev), torch.empty((T, k), dtype=i32, device=dev)
+        out = (gates, experts, offsets, row_token, slot_row)
+    else:
+        gates, experts, offsets, row_token, slot_row = out
+        _dense(gates, (T, k), torch.float32, "gates"), _dense(experts, (T, k), i32, "experts"), _dense(offsets, (E + 1,), i32, "offsets")
+        _dense(row_token, (T * k,), i32, "row_token"), _dense(slot_row, (T, k), i32, "slot_row")
     _check(load_library().fast_moe_route(logits, T, E, ld, k, flags, gates, experts, offsets, row_token, slot_row, workspace,
                                          workspace.numel(), _stream()))
     return out
@@ -917,11 +922,27 @@ def fp8_grouped_linear_fwd_prequantized(x: torch.Tensor, wq: torch.Tensor, fmt_w
 FP8_ADAMW_BLOCK = 256
 
 
-class AdamwTensors:
-    """The tensors of an AdamW step as the library reads them; made once, kept with the parameters (and keeps them)."""
+def fp8_adamw_table_bytes(tensors, count: int, flags: int) -> int:
+    """tensors: a ctypes array of descriptors."""
+    n = load_library().fp8_adamw_table_bytes(C.addressof(tensors), count, flags)
+    if n == 0:
+        raise Fp8Error(-2, fp8_last_error())
+    return int(n)
 
-    def __init__(self, array, count: int, flags: int, tensors):
-        self.array, self.count, self.flags, self.tensors = array, count, flags, tensors
+
+def fp8_adamw_table(tensors, count: int, flags: int):
+    """(the table in host memory, the launch's blocks) of a ctypes array of descriptors."""
+    table, blocks = torch.empty(fp8_adamw_table_bytes(tensors, count, flags), dtype=torch.uint8), C.c_int64(0)
+    _check(load_library().fp8_adamw_table(C.addressof(tensors), count, flags, table.data_ptr(), table.numel(), C.byref(blocks)))
+    return table, blocks.value
+
+
+class AdamwTensors:
+    """The tensors of an AdamW step as the library reads them: made once, kept with the parameters.  Holds the tensors, which must
+    stay where they are."""
+
+    def __init__(self, table: torch.Tensor, blocks: int, flags: int, tensors):
+        self.table, self.blocks, self.flags, self.tensors = table, blocks, flags, tensors
 
 
 def fp8_adamw_tensors(params, grads, exp_avg, exp_avg_sq, scale_m=None, scale_v=None) -> AdamwTensors:
@@ -955,12 +976,13 @@ def fp8_adamw_tensors(params, grads, exp_avg, exp_avg_sq, scale_m=None, scale_v=
             f"tensor {i}: sizes {[t.numel() for t in ts]}"
         ptrs = [t.data_ptr() if size else None for t in ts] + [None] * (6 - len(ts))
         array[i] = _CAdamwTensor(*ptrs, size)
-    return AdamwTensors(array, n, flags, lists)
+    table, blocks = fp8_adamw_table(array, n, flags)
+    return AdamwTensors(table.to(lists[0][0].device) if n else table, blocks, flags, lists)
 
 
 def fp8_adamw_step(tensors: AdamwTensors, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
                    weight_decay: float = 0.01, grad_scale: torch.Tensor | None = None) -> None:
     """One AdamW step in place over all of them.  grad_scale: one float32 on the GPU that multiplies the gradients."""
     assert grad_scale is None or (grad_scale.is_cuda and grad_scale.dtype == torch.float32 and grad_scale.numel() == 1)
-    _check(load_library().fp8_adamw_step(C.addressof(tensors.array), tensors.count, tensors.flags, lr, beta1, beta2, eps, weight_decay, step,
+    _check(load_library().fp8_adamw_step(_ptr(tensors.table), tensors.blocks, tensors.flags, lr, beta1, beta2, eps, weight_decay, step,
                                          _ptr(grad_scale), _stream()))

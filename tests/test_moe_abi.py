@@ -128,10 +128,16 @@ def test_grouped_linear(lib, p):
     assert lib.fp8_grouped_linear_prequantized_workspace_bytes(8, 24) == 0
 
 
-def test_adamw(lib, p):
-    def call(fields=(p, p, p, p, p, p, 8), count=1, flags=fp8.FP8_ADAMW_STATE_FP8, lr=1e-3, b1=0.9, b2=0.99, eps=1e-8, wd=0.1, step=1, scale=None, none=False):
+def test_adamw_table(lib, p):
+    q = fp8.FP8_ADAMW_STATE_FP8
+
+    def call(fields=(p, p, p, p, p, p, 8), count=1, flags=q, none=False, table=p, n=4096):
         t = (_CAdamwTensor * 1)(_CAdamwTensor(*fields))
-        return lib.fp8_adamw_step(None if none else C.addressof(t), count, flags, lr, b1, b2, eps, wd, step, scale, None)
+        blocks = C.c_int64(-7)
+        at = None if none else C.addressof(t)
+        rc = lib.fp8_adamw_table(at, count, flags, table, n, C.byref(blocks))
+        assert (lib.fp8_adamw_table_bytes(at, count, flags) > 0) == (rc in (0, WORKSPACE) or table is None)
+        return rc if rc else ("ok", blocks.value)
 
     for i in range(6):
         f = [p, p, p, p, p, p, 8]
@@ -139,9 +145,37 @@ def test_adamw(lib, p):
         assert call(f) == NULL, i
         f[i] = p + (8 if i < 4 else 2)
         assert call(f) == ALIGN, i
-    assert call((p, p, p, p, p, p, -1)) == SHAPE and "tensor 0" in fp8.fp8_last_error()
-    assert call((None,) * 6 + (0,)) == 0 and call(count=0) == 0 and call(none=True) == NULL and call(count=-1) == SHAPE
+    assert call((p, p, p, p, p, p, -1)) == SHAPE and call((p, p, p, p, p, p, 1 << 38)) == SHAPE
+    assert call((None,) * 6 + (0,)) == ("ok", 0) and call(count=0) == ("ok", 0) and call(none=True) == NULL and call(count=-1) == SHAPE
+    assert call((p, p, p, p, None, None, 8), flags=0) == ("ok", 1)
+    assert call(flags=1) == ENUM and call(table=None) == NULL and call(n=8) == WORKSPACE
+    assert lib.fp8_adamw_table(p, 0, 0, p, 4096, None) == NULL
+
+
+@pytest.mark.parametrize("sizes", [[1], [2048, 2049, 0, 5], [16384 * 2048, 1], [16384 * 2048 + 1, 8193, 0, 3]])
+def test_adamw_table_covers_every_element_once(sizes):
+    """Header (count, blocks, flags and rounds), the tensors, then (tensor, piece) of each workgroup; a piece is rounds * 2048."""
+    import numpy as np
+    array = (_CAdamwTensor * len(sizes))(*[_CAdamwTensor(4096, 4096, 4096, 4096, None, None, n) for n in sizes])
+    table, blocks = fp8.fp8_adamw_table(array, len(sizes), 0)
+    raw = table.numpy()
+    count, n_blocks = raw[:16].view(np.int64)
+    flags, rounds = raw[16:24].view(np.int32)
+    assert (count, n_blocks, flags) == (len(sizes), blocks, 0)
+    assert rounds == (1 if sum(-(-n // 2048) for n in sizes) <= 16384 else 4)
+    pieces = raw[32 + 56 * len(sizes):].view(np.int32).reshape(-1, 2)
+    assert len(pieces) == blocks
+    want = [(i, j) for i, n in enumerate(sizes) for j in range(-(-n // (2048 * rounds)))]
+    assert [tuple(x) for x in pieces] == want
+    assert raw[32 + 48:32 + 56].view(np.int64)[0] == sizes[0]
+
+
+def test_adamw_step(lib, p):
+    def call(table=p, blocks=1, flags=0, lr=1e-3, b1=0.9, b2=0.99, eps=1e-8, wd=0.1, step=1, scale=None):
+        return lib.fp8_adamw_step(table, blocks, flags, lr, b1, b2, eps, wd, step, scale, None)
+
     nan = float("nan")
-    for bad in ({"lr": -1.0}, {"lr": nan}, {"b1": 1.0}, {"b1": nan}, {"b2": -0.1}, {"eps": -1.0}, {"wd": -1.0}, {"step": 0}):
+    for bad in ({"lr": -1.0}, {"lr": nan}, {"b1": 1.0}, {"b1": nan}, {"b2": -0.1}, {"eps": -1.0}, {"wd": -1.0}, {"step": 0}, {"blocks": -1}, {"blocks": 1 << 24}):
         assert call(**bad) == SHAPE, bad
-    assert call(flags=1) == ENUM and call(scale=p + 1) == ALIGN
+    assert call(flags=1) == ENUM and call(scale=p + 1) == ALIGN and call(table=None) == NULL and call(table=p + 8) == ALIGN
+    assert call(blocks=0) == 0
