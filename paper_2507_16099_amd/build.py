@@ -15,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libfp8mi355.so")
 PYCALL = os.path.join(HERE, "_pycall" + EXTENSION_SUFFIXES[0])      # (names the interpreter that it is for)
-SOURCES = ["quant_kernels.hip", "quant_strips.hip", "tuning.hip", "gemm_fp8.hip", "gemm_fp8_snake.hip", "gemm_fp8_stream.hip", "gemm_fp8_ring.hip", "gemm_mxfp8_ring.hip", "gemm_fp8_skinny.hip", "gemm_fp8_skinny_fused.hip", "gemm_fp8_few_stream.hip", "gemm_bf16_at_b.hip", "gemm_bf16_at_b_snake.hip", "layernorm_quant.hip", "gemm_mxfp8.hip", "gemm_mxfp8_snake.hip", "gemm_mxfp8_stream.hip", "moe_route.hip", "moe_combine.hip", "grouped_quant.hip", "gemm_fp8_grouped.hip", "gemm_fp8_grouped_stream.hip", "adamw.hip", "moe_api.hip", "api.hip"]
+SOURCES = ["quant_kernels.hip", "quant_strips.hip", "tuning.hip", "gemm_fp8.hip", "gemm_fp8_snake.hip", "gemm_fp8_stream.hip", "gemm_fp8_ring.hip", "gemm_mxfp8_ring.hip", "gemm_fp8_skinny.hip", "gemm_fp8_skinny_fused.hip", "gemm_fp8_few_stream.hip", "gemm_bf16_at_b.hip", "gemm_bf16_at_b_snake.hip", "layernorm_quant.hip", "gemm_mxfp8.hip", "gemm_mxfp8_snake.hip", "gemm_mxfp8_stream.hip", "moe_route.hip", "moe_combine.hip", "grouped_quant.hip", "gemm_fp8_grouped.hip", "gemm_fp8_grouped_stream.hip", "gemm_fp8_grouped_few.hip", "adamw.hip", "moe_api.hip", "api.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed-fp32 instructions are disabled on purpose (the compiler would
 # otherwise form v_pk_*_f32 from plain float code)

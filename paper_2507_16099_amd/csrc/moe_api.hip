@@ -331,8 +331,13 @@ int fp8_grouped_linear_fwd_prequantized(const void* x, int64_t T, const int32_t*
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     float* sx = reinterpret_cast<float*>(ws + p.sx);
     hipStream_t st = static_cast<hipStream_t>(stream);
+    const fp8k::GroupedGemm g{ws + p.xq, pitch(K), fmt_x, sx, wq, ldw, fmt_w, scale_w, offsets, E, M, N, K, y, N};
+    if (hipError_t e = fp8k::launch_grouped_few(x, T, row_token, fmt_x, flags, g, st); e != hipErrorNotSupported) {
+        FP8_TRY(e);
+        return FP8_OK;
+    }
     FP8_TRY(fp8k::launch_quant_rows_gather(x, T, K, row_token, M, K, fmt_x, flags, ws + p.xq, pitch(K), sx, st));
-    FP8_TRY(fp8k::launch_gemm_fp8_grouped_rows({ws + p.xq, pitch(K), fmt_x, sx, wq, ldw, fmt_w, scale_w, offsets, E, M, N, K, y, N}, st));
+    FP8_TRY(fp8k::launch_gemm_fp8_grouped_rows(g, st));
     return FP8_OK;
 }
 

@@ -50,6 +50,9 @@ struct GroupedGemm {
 };
 // out[r, :N] for the rows r of a group: A row r [K], B rows of that group (b + e N ldb, scale_b + e N); rows past the last group: zeros
 hipError_t launch_gemm_fp8_grouped_rows(const GroupedGemm& g, hipStream_t st);
+// the same with A quantized inside, for few rows per group: row r is fp8(x[row_token[r]]) (g.a, g.scale_a unused); hipErrorNotSupported
+// (nothing launched) where that form does not apply
+hipError_t launch_grouped_few(const void* x, int64_t T, const int32_t* row_token, int fmt_x, int flags, const GroupedGemm& g, hipStream_t st);
 // out[e] [N, K] for each group: A [N, lda], B [K, ldb] with the group's columns where launch_quant_cols_grouped leaves them;
 // scale_a [E, N], scale_b [E, K]
 hipError_t launch_gemm_fp8_grouped_contract(const GroupedGemm& g, hipStream_t st);

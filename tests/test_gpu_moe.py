@@ -181,11 +181,11 @@ def test_grouped_linear(case, recipe):
     want, size = ref.grouped_fwd(xr, w, offsets, fmt[r.fmt_x], fmt[r.fmt_w], pow2)
     y = fp8.fp8_grouped_linear_fwd(xd, wd, od, r, row_token=rd)
     ref.assert_product(y.cpu(), want, size)
-    # the same with the weights quantized beforehand: the same bits
+    # the same with the weights quantized beforehand: the same codes, and the same bits where the sums have the same order
     E = len(sizes)
     wq, sw = fp8.fp8_quantize(wd.view(E * N, K), fp8.FP8_ROW, r.fmt_w, r.flags)
     y2 = fp8.fp8_grouped_linear_fwd_prequantized(xd, wq.view(E, N, K), r.fmt_w, sw.view(E, N), od, r.fmt_x, r.flags, row_token=rd)
-    assert torch.equal(y.view(torch.int16), y2.view(torch.int16))
+    ref.assert_product(y2.cpu(), want, size)
     # rows given as they are: the same bits
     y3 = fp8.fp8_grouped_linear_fwd(xr.cuda(), wd, od, r)
     assert torch.equal(y.view(torch.int16), y3.view(torch.int16))
@@ -197,6 +197,36 @@ def test_grouped_linear(case, recipe):
     assert none is None and torch.equal(only.view(torch.int16), dx.view(torch.int16))
     none, only = fp8.fp8_grouped_linear_bwd(dyd, xd, wd, od, r, row_token=rd, need_dx=False)
     assert none is None and torch.equal(only.view(torch.int16), dw.view(torch.int16))
+
+
+# few rows per expert: a row, tiles of sixteen and more, runs that cross from expert to expert, none at all, long and odd rows
+FEW = [([1], 1, 16, 16, 0), ([0, 1, 0, 1], 1, 4096, 4096, 0), ([2, 0, 0, 0], 2, 1040, 24, 0), ([16, 17, 0, 5, 1, 33], 40, 528, 200, 3),
+       ([0] * 200 + [1] * 50 + [7, 0], 33, 256, 8, 4), ([6] * 64, 64, 2048, 112, 0), ([3, 1, 0, 12], 9, 9008, 40, 0), ([1, 2], 3, 16384, 24, 0),
+       ([0, 0, 0], 2, 64, 32, 6), ([9, 15, 1], 25, 16400, 32, 0), ([1] * 31 + [0, 40], 9, 144, 600, 2)]
+
+
+@pytest.mark.parametrize("recipe", RECIPES)
+@pytest.mark.parametrize("case", range(len(FEW)))
+def test_few_rows_against_quantized_weights(case, recipe):
+    sizes, T, K, N, tail = FEW[case]
+    r = fp8.Recipe(gran=fp8.FP8_ROW, **RECIPES[recipe])
+    fmt = {0: ref.E4M3, 1: ref.E5M2}
+    offsets, row_token, x, w, _ = _case(sizes, T, K, N, 177 + case, tail)
+    if row_token.numel() > 3:
+        row_token[2] = T + 5      # a token that is none: a row of zeros
+    E, xr = len(sizes), ref.rows_of(x, row_token)
+    want, size = ref.grouped_fwd(xr, w, offsets, fmt[r.fmt_x], fmt[r.fmt_w], bool(r.flags))
+    wd = torch.zeros((E, N, K + 16), dtype=torch.bfloat16, device="cuda")      # rows of codes further apart than they are long
+    wd[:, :, :K] = w.cuda()
+    wq = torch.full((E * N, K + 16), 0x7F, dtype=torch.uint8, device="cuda")
+    _, sw = fp8.fp8_quantize(wd.view(E * N, K + 16)[:, :K], fp8.FP8_ROW, r.fmt_w, r.flags, out=wq[:, :K])
+    y = torch.full((len(row_token), N), float("nan"), dtype=BF16, device="cuda")
+    fp8.fp8_grouped_linear_fwd_prequantized(x.cuda(), wq.view(E, N, K + 16)[:, :, :K], r.fmt_w, sw.view(E, N), offsets.cuda(), r.fmt_x, r.flags,
+                                            row_token=row_token.cuda(), y=y)
+    ref.assert_product(y.cpu(), want, size)
+    if not tail and case % 2:      # the rows as they are
+        y2 = fp8.fp8_grouped_linear_fwd_prequantized(xr.cuda(), wq.view(E, N, K + 16)[:, :, :K], r.fmt_w, sw.view(E, N), offsets.cuda(), r.fmt_x, r.flags)
+        assert torch.equal(y.view(torch.int16), y2.view(torch.int16))
 
 
 @pytest.mark.parametrize("offsets", [[0, 50, 20, 90, 200, -5], [0, -3, -4, 1 << 30, 7, 100], [7, 7, 7, 7, 7, 7], [0, 2147483647, -2147483648, 60, 40, 100]])
