@@ -66,8 +66,7 @@ __global__ __launch_bounds__(st::NT) void gemm_fp8_grouped_stream_kernel(Grouped
             int g_end = e < p.E ? p.offsets[e + 1] : e == p.E ? p.M : 0;
             g_end = g_end < end ? end : g_end > p.M ? p.M : g_end;
             g_end = wave_scan_max(g_end);
-            int g_start = __shfl_up(g_end, 1, 64);
-            if (lane == 0) g_start = end;
+            const int g_start = wave_before(g_end, end);
             const int tiles = (g_end - g_start + TM - 1) / TM, pad = (g_end - g_start + 127) & ~127;
             const int tiles_sum = tiles_before + wave_scan_add(tiles), pad_sum = pad_before + wave_scan_add(pad);
             if (e <= p.E) {
@@ -79,9 +78,9 @@ __global__ __launch_bounds__(st::NT) void gemm_fp8_grouped_stream_kernel(Grouped
                 starts[e + 1] = g_end;
                 tiles_to[e + 1] = tiles_sum;
             }
-            end = __shfl(g_end, 63, 64);
-            tiles_before = __shfl(tiles_sum, 63, 64);
-            pad_before = __shfl(pad_sum, 63, 64);
+            end = at_lane(g_end, 63);
+            tiles_before = at_lane(tiles_sum, 63);
+            pad_before = at_lane(pad_sum, 63);
         }
     }
     __syncthreads();

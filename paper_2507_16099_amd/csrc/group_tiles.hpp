@@ -9,25 +9,29 @@
 
 namespace fp8k {
 
-// inclusive scans over the 64 lanes
+// Inclusive scans over the 64 lanes in registers: shifts by 1, 2, 4, 8 within the rows of 16, then the last lane of a row to the next
+// row and that of the first half to the second.
+template <class F>
+__device__ __forceinline__ int wave_scan(int v, int none, F f) {
+    v = f(v, __builtin_amdgcn_update_dpp(none, v, 0x111, 0xF, 0xF, false));      // row_shr:1, 2, 4, 8
+    v = f(v, __builtin_amdgcn_update_dpp(none, v, 0x112, 0xF, 0xF, false));
+    v = f(v, __builtin_amdgcn_update_dpp(none, v, 0x114, 0xF, 0xF, false));
+    v = f(v, __builtin_amdgcn_update_dpp(none, v, 0x118, 0xF, 0xF, false));
+    v = f(v, __builtin_amdgcn_update_dpp(none, v, 0x142, 0xA, 0xF, false));      // row_bcast:15 into rows 1 and 3
+    v = f(v, __builtin_amdgcn_update_dpp(none, v, 0x143, 0xC, 0xF, false));      // row_bcast:31 into rows 2 and 3
+    return v;
+}
 __device__ __forceinline__ int wave_scan_add(int v) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(v, d, 64);
-        if (lane >= d) v += o;
-    }
-    return v;
+    return wave_scan(v, 0, [](int a, int b) { return a + b; });
 }
-__device__ __forceinline__ int wave_scan_max(int v) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(v, d, 64);
-        if (lane >= d) v = o > v ? o : v;
-    }
-    return v;
+__device__ __forceinline__ int wave_scan_max(int v) {      // of numbers that are not negative
+    return wave_scan(v, 0, [](int a, int b) { return a > b ? a : b; });
 }
+// the lane before, lane 0 gets `first`
+__device__ __forceinline__ int wave_before(int v, int first) { return __builtin_amdgcn_update_dpp(first, v, 0x138, 0xF, 0xF, false); }      // wave_shr:1
+
+// the value of one lane, the same lane for all
+__device__ __forceinline__ int at_lane(int v, int l) { return __builtin_amdgcn_readlane(v, __builtin_amdgcn_readfirstlane(l)); }
 
 struct GroupTile {
     int group;       // E: the rows behind the last group
@@ -49,24 +53,23 @@ __device__ __forceinline__ GroupTile find_group_tile(const int32_t* __restrict__
         int b = e < E ? offsets[e + 1] : TAIL && e == E ? M : 0;
         b = b < end ? end : b > M ? M : b;
         b = wave_scan_max(b);
-        int a = __shfl_up(b, 1, 64);
-        if (lane == 0) a = end;
+        const int a = wave_before(b, end);
         const int n = b - a, tiles = (n + height - 1) / height, pad = (n + 127) & ~127;
         const int tiles_to = tiles_before + wave_scan_add(tiles), pad_to = pad_before + wave_scan_add(pad);
         const uint64_t hit = __ballot(index >= 0 && index < tiles_to);
         if (t.group < 0 && hit) {
             const int l = __ffsll((unsigned long long)hit) - 1;
-            const int in = index - (__shfl(tiles_to, l, 64) - __shfl(tiles, l, 64));
-            const int a_l = __shfl(a, l, 64), n_l = __shfl(n, l, 64);
+            const int in = index - (at_lane(tiles_to, l) - at_lane(tiles, l));
+            const int a_l = at_lane(a, l), n_l = at_lane(n, l);
             t.group = e0 + l;
             t.row0 = a_l + in * height;
             t.first = in == 0;
             t.rows = n_l - in * height < height ? n_l - in * height : height;
-            t.pad0 = __shfl(pad_to, l, 64) - __shfl(pad, l, 64) + in * height;
+            t.pad0 = at_lane(pad_to, l) - at_lane(pad, l) + in * height;
         }
-        end = __shfl(b, 63, 64);
-        tiles_before = __shfl(tiles_to, 63, 64);
-        pad_before = __shfl(pad_to, 63, 64);
+        end = at_lane(b, 63);
+        tiles_before = at_lane(tiles_to, 63);
+        pad_before = at_lane(pad_to, 63);
     }
     t.total = tiles_before;
     t.group = __builtin_amdgcn_readfirstlane(t.group);
@@ -88,18 +91,17 @@ __device__ __forceinline__ GroupSpan find_group(const int32_t* __restrict__ offs
         int b = e < E ? offsets[e + 1] : 0;
         b = b < end ? end : b > M ? M : b;
         b = wave_scan_max(b);
-        int a = __shfl_up(b, 1, 64);
-        if (lane == 0) a = end;
+        const int a = wave_before(b, end);
         const int pad = (b - a + 127) & ~127;
         const int pad_to = pad_before + wave_scan_add(pad);
         if (group < e0 + 64) {
             const int l = group - e0;
-            s.row0 = __shfl(a, l, 64);
-            s.rows = __shfl(b - a, l, 64);
-            s.pad0 = __shfl(pad_to, l, 64) - __shfl(pad, l, 64);
+            s.row0 = at_lane(a, l);
+            s.rows = at_lane(b - a, l);
+            s.pad0 = at_lane(pad_to, l) - at_lane(pad, l);
         }
-        end = __shfl(b, 63, 64);
-        pad_before = __shfl(pad_to, 63, 64);
+        end = at_lane(b, 63);
+        pad_before = at_lane(pad_to, 63);
     }
     s.row0 = __builtin_amdgcn_readfirstlane(s.row0);
     s.rows = __builtin_amdgcn_readfirstlane(s.rows);
