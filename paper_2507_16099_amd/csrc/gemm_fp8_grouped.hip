@@ -300,13 +300,29 @@ hipError_t launch_t(const GroupedGemm& g, hipStream_t st) {
     return hipGetLastError();
 }
 
+// the tile forms (of RingTile, launchers.hpp): height, width, stages, tile rows walked together
+template <int FA, int FB, bool CONTRACT>
+hipError_t launch_tile(int tile, const GroupedGemm& g, hipStream_t st) {
+    switch (tile) {
+        case RING_64x64: return launch_t<FA, FB, 64, 64, 2, 2, 4, 4, CONTRACT>(g, st);
+        case RING_128x64: return launch_t<FA, FB, 128, 64, 2, 2, 3, 4, CONTRACT>(g, st);
+        case RING_64x128: return launch_t<FA, FB, 64, 128, 2, 2, 4, 8, CONTRACT>(g, st);
+        case RING_128x256: return launch_t<FA, FB, 128, 256, 2, 2, 3, 8, CONTRACT>(g, st);
+        case RING_96x128: return launch_t<FA, FB, 96, 128, 2, 2, 4, 8, CONTRACT>(g, st);
+        case RING_192x128: return launch_t<FA, FB, 192, 128, 2, 2, 3, 4, CONTRACT>(g, st);
+        case RING_256x128: return launch_t<FA, FB, 256, 128, 2, 2, 3, 4, CONTRACT>(g, st);
+        default: return launch_t<FA, FB, 128, 128, 2, 2, 4, 4, CONTRACT>(g, st);
+    }
+}
+
 template <int FA, int FB>
 hipError_t launch_rows(const GroupedGemm& g, hipStream_t st) {
     const int64_t mean = g.M / g.E;
-    if (mean >= 256 && gemm_fp8_grouped_stream_fits(g)) return launch_gemm_fp8_grouped_stream_rows(g, st);
+    const int ring = knob(KNOB_GEMM_RING), stream = knob(KNOB_GEMM_STREAM);
+    if (ring > 0) return launch_tile<FA, FB, false>(ring - 1, g, st);
+    if ((stream >= 2 || (stream != 0 && mean >= 256)) && gemm_fp8_grouped_stream_fits(g)) return launch_gemm_fp8_grouped_stream_rows(g, st);
     if (mean <= 16) return launch_t<FA, FB, 32, 128, 1, 4, 6, 1, false>(g, st);
-    if (mean <= 64) return launch_t<FA, FB, 64, 128, 2, 2, 4, 8, false>(g, st);
-    return launch_t<FA, FB, 128, 128, 2, 2, 4, 4, false>(g, st);
+    return launch_tile<FA, FB, false>(mean <= 64 ? RING_64x128 : RING_128x128, g, st);
 }
 
 }  // namespace
@@ -324,8 +340,10 @@ hipError_t launch_gemm_fp8_grouped_rows(const GroupedGemm& g, hipStream_t st) {
 
 template <int FA, int FB>
 static hipError_t launch_contract(const GroupedGemm& g, hipStream_t st) {
-    if (gemm_fp8_grouped_stream_fits(g)) return launch_gemm_fp8_grouped_stream_contract(g, st);
-    return launch_t<FA, FB, 128, 128, 2, 2, 4, 4, true>(g, st);
+    const int ring = knob(KNOB_GEMM_RING);
+    if (ring > 0) return launch_tile<FA, FB, true>(ring - 1, g, st);
+    if (knob(KNOB_GEMM_STREAM) != 0 && gemm_fp8_grouped_stream_fits(g)) return launch_gemm_fp8_grouped_stream_contract(g, st);
+    return launch_tile<FA, FB, true>(RING_128x128, g, st);
 }
 hipError_t launch_gemm_fp8_grouped_contract(const GroupedGemm& g, hipStream_t st) { FP8K_FORMATS(launch_contract) }
 

@@ -155,8 +155,8 @@ __global__ __launch_bounds__(64 * WAVES) void grouped_few_kernel(FewArgs p) {
             return make_uint4(real ? v.x : 0u, real ? v.y : 0u, real ? v.z : 0u, real ? v.w : 0u);
         };
         // (without these the compiler requests all pieces of a long row at once, and spills)
-        auto every_other = [&](int s) {
-            if (s % 2 == 1) {
+        auto every_fourth = [&](int s) {
+            if (s % 4 == 3) {
                 asm volatile("" ::: "memory");
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -176,7 +176,7 @@ __global__ __launch_bounds__(64 * WAVES) void grouped_few_kernel(FewArgs p) {
             }
             if constexpr (!KEEP) {
                 asm volatile("" : "+v"(m));
-                every_other(s);
+                every_fourth(s);
             }
         }
         if constexpr (KEEP) {
@@ -201,7 +201,7 @@ __global__ __launch_bounds__(64 * WAVES) void grouped_few_kernel(FewArgs p) {
             af[st] = v8i_g{(int)q[0].x, (int)q[0].y, (int)q[1].x, (int)q[1].y, (int)q[2].x, (int)q[2].y, (int)q[3].x, (int)q[3].y};
             if constexpr (!KEEP) {
                 asm volatile("" : "+v"(af[st]));
-                every_other(st);
+                every_fourth(st);
             }
         }
     };
@@ -267,7 +267,8 @@ hipError_t launch_t(const FewArgs& a, int64_t grid, hipStream_t st) {
 
 // hipErrorNotSupported (nothing launched): more rows, or a longer contraction, than it is for
 hipError_t launch_grouped_few(const void* x, int64_t T, const int32_t* row_token, int fmt_x, int flags, const GroupedGemm& g, hipStream_t st) {
-    if (g.M > 16 * g.E || g.K > 16384 || T < 1) return hipErrorNotSupported;
+    const int forced = knob(KNOB_SKINNY_DMA);      // 0: never, 2: whatever the number of rows
+    if (forced == 0 || (g.M > 16 * g.E && forced < 2) || g.K > 16384 || T < 1) return hipErrorNotSupported;
     const int64_t cus = compute_units() > 0 ? compute_units() : 256;
     const int64_t tiles_n = (g.N + 15) / 16, most = (g.M / 16 + (g.E + 1 < g.M ? g.E + 1 : g.M)) * tiles_n;
     if (most > 0x3FFFFFFF) return hipErrorNotSupported;

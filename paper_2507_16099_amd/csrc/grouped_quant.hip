@@ -15,6 +15,15 @@ namespace fp8k {
 
 namespace {
 
+// Workgroups are dealt to the eight XCDs in turn.  Number of the workgroup in an order that gives each XCD a contiguous range of `total`,
+// so that pieces of the same rows are read by the same XCD at about the same time (-1: beyond the last; the grid is a multiple of 8).
+// Column strips of 64 experts' weights 1408 x 2048, 32 columns a strip, one expert's strips on all XCDs 156 us, on one 123.
+__device__ __forceinline__ int xcd_order(int total) {
+    const int per = (total + 7) / 8, slot = (int)blockIdx.x >> 3, b = ((int)blockIdx.x & 7) * per + slot;
+    return slot < per && b < total ? b : -1;
+}
+unsigned xcd_grid(int64_t total) { return (unsigned)((total + 7) / 8 * 8); }
+
 // ---- rows -----------------------------------------------------------------------------------------------------------
 
 // one workgroup per row, the row in registers (NV pieces of eight per thread); NV == 0: any length, read twice
@@ -85,9 +94,10 @@ struct ColArgs {
     const uint16_t* x;
     int64_t T, ldx;
     const int32_t *row_token, *offsets;      // offsets nullptr: groups of M / E rows
-    int M, E, cols, flags;
+    int M, E, cols, flags, keep;             // keep: codes through the L2, else past the caches (keep_codes)
     uint8_t* qt;
     int64_t ld_t, group_stride;
+    int tiles;                               // tiles of 128 rows that the groups can come to
     float* scale;
     uint32_t* amax;
 };
@@ -98,29 +108,41 @@ __device__ __forceinline__ GroupTile tile_of(const ColArgs& a, int height, int i
     return GroupTile{e < a.E ? e : -1, e * n + in * height, n - in * height < height ? n - in * height : height, in * height, per * a.E, in == 0};
 }
 
-// the row of x behind row r, or nullptr
-__device__ __forceinline__ const uint16_t* row_of(const ColArgs& a, int r) {
-    const int64_t t = a.row_token ? a.row_token[r] : r;
-    return t >= 0 && t < a.T ? a.x + t * a.ldx : nullptr;
+// Rows of x behind `n` rows from row0 on, into LDS (-1: none), by the whole workgroup.  From there the loads of a tile's rows are
+// requested together; a lookup in memory in front of each of them makes every load wait for the one before it.
+__device__ __forceinline__ void list_rows(const ColArgs& a, int row0, int n, int* list) {
+    for (int r = threadIdx.x; r < n; r += blockDim.x) {
+        const int64_t t = a.row_token ? a.row_token[row0 + r] : row0 + r;
+        list[r] = t >= 0 && t < a.T ? (int)t : -1;
+    }
+    __syncthreads();
+}
+// eight elements of column c on of that row, zeros where there are none (read from x's first row all the same: no branch)
+__device__ __forceinline__ uint4 piece_of(const ColArgs& a, int row, int c) {
+    const bool real = row >= 0 && c < a.cols;
+    const uint4 v = *reinterpret_cast<const uint4*>(a.x + (real ? row : 0) * a.ldx + (real ? c : 0));
+    return make_uint4(real ? v.x : 0u, real ? v.y : 0u, real ? v.z : 0u, real ? v.w : 0u);
 }
 
 // Maxima: a workgroup takes 512 columns (a lane eight) of up to HEIGHT rows of a group, a wavefront every fourth row.
 constexpr int AMAX_ROWS = 128;
 __global__ __launch_bounds__(256) void cols_amax_kernel(ColArgs a) {
     __shared__ uint4 part[4][64];
-    const GroupTile t = tile_of(a, AMAX_ROWS, blockIdx.x);
+    const int strips = (a.cols + 511) / 512, b = xcd_order(a.tiles * strips);
+    if (b < 0) return;
+    const GroupTile t = tile_of(a, AMAX_ROWS, b / strips);
     if (t.group < 0) return;
+    const int col0 = (b % strips) * 512;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int c = (int)blockIdx.y * 512 + lane * 8;
+    const int c = col0 + lane * 8;
+    __shared__ int list[AMAX_ROWS];
+    list_rows(a, t.row0, t.rows, list);
     uint4 m = make_uint4(0, 0, 0, 0);
     if (c < a.cols) {
         for (int r0 = wave; r0 < t.rows; r0 += 32) {
             uint4 v[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint16_t* row = r0 + 4 * i < t.rows ? row_of(a, t.row0 + r0 + 4 * i) : nullptr;
-                v[i] = row ? *reinterpret_cast<const uint4*>(row + c) : make_uint4(0, 0, 0, 0);
-            }
+            for (int i = 0; i < 8; ++i) v[i] = piece_of(a, r0 + 4 * i < t.rows ? list[r0 + 4 * i] : -1, c);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 m.x = pk_absmax(m.x, v[i].x); m.y = pk_absmax(m.y, v[i].y);
@@ -135,7 +157,7 @@ __global__ __launch_bounds__(256) void cols_amax_kernel(ColArgs a) {
     uint32_t w = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) w = pk_absmax(w, reinterpret_cast<const uint32_t*>(&part[i][l])[d]);
-    const int col = (int)blockIdx.y * 512 + l * 8 + d * 2;
+    const int col = col0 + l * 8 + d * 2;
     if (col < a.cols) {
         uint32_t* to = a.amax + (int64_t)t.group * a.cols + col;
         atomicMax(to, w & 0xFFFFu);
@@ -149,32 +171,34 @@ __global__ __launch_bounds__(256) void cols_amax_kernel(ColArgs a) {
 template <int FMT>
 __global__ __launch_bounds__(256) void cols_cast_kernel(ColArgs a) {
     __shared__ __attribute__((aligned(16))) uint8_t turned[128 * 128];
-    const GroupTile t = tile_of(a, 128, blockIdx.x);
+    const int strips = (a.cols + 127) / 128, b = xcd_order(a.tiles * strips);
+    if (b < 0) return;
+    const GroupTile t = tile_of(a, 128, b / strips);
     if (t.group < 0) return;
     const int tid = threadIdx.x, p = tid >> 4, l = tid & 15;
-    const int c = (int)blockIdx.y * 128 + l * 8;
+    const int col0 = (b % strips) * 128, c = col0 + l * 8;
+    __shared__ int list[128];
+    list_rows(a, t.row0, t.rows, list);
     uint4 v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int r = 4 * p + (i & 3) + 64 * (i >> 2);
-        const uint16_t* row = c < a.cols && r < t.rows ? row_of(a, t.row0 + r) : nullptr;
-        v[i] = row ? *reinterpret_cast<const uint4*>(row + c) : make_uint4(0, 0, 0, 0);
+        v[i] = piece_of(a, r < t.rows ? list[r] : -1, c);
     }
+    // one column's scale per thread; the group's first tile of rows leaves them for the product
+    __shared__ __attribute__((aligned(16))) float scales[128];
+    if (tid < 128) {
+        const int col = col0 + tid;
+        const int64_t at = (int64_t)t.group * a.cols + col;
+        const float s = col < a.cols ? scale_from_amax(mag_to_float(a.amax[at]), FMT, a.flags) : 0.f;
+        scales[tid] = s;
+        if (t.first && col < a.cols) a.scale[at] = s;
+    }
+    __syncthreads();
     float s[8];
-    if (c < a.cols) {
-        const int64_t at = (int64_t)t.group * a.cols + c;
-        const uint4 m0 = *reinterpret_cast<const uint4*>(a.amax + at), m1 = *reinterpret_cast<const uint4*>(a.amax + at + 4);
-        const uint32_t m[8] = {m0.x, m0.y, m0.z, m0.w, m1.x, m1.y, m1.z, m1.w};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] = scale_from_amax(mag_to_float(m[e]), FMT, a.flags);
-        // (the group's first tile of rows leaves them for the product)
-        if (t.first && p == 0) {
-#pragma unroll
-            for (int e = 0; e < 8; e += 4) *reinterpret_cast<float4*>(a.scale + at + e) = make_float4(s[e], s[e + 1], s[e + 2], s[e + 3]);
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] = 0.f;
+    {
+        const float4 s0 = *reinterpret_cast<const float4*>(scales + l * 8), s1 = *reinterpret_cast<const float4*>(scales + l * 8 + 4);
+        s[0] = s0.x; s[1] = s0.y; s[2] = s0.z; s[3] = s0.w; s[4] = s1.x; s[5] = s1.y; s[6] = s1.z; s[7] = s1.w;
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -201,9 +225,153 @@ __global__ __launch_bounds__(256) void cols_cast_kernel(ColArgs a) {
     for (int i = 0; i < 4; ++i) {
         const int col = i * 32 + (tid >> 3), piece = tid & 7;
         const uint4 w = *reinterpret_cast<const uint4*>(turned + col * 128 + ((piece ^ ((col >> 3) & 7)) << 4));
-        if ((int)blockIdx.y * 128 + col < a.cols && piece * 16 < rows16)
-            store_vec(a.qt + t.group * a.group_stride + (int64_t)((int)blockIdx.y * 128 + col) * a.ld_t + t.pad0 + piece * 16, w);
+        if (col0 + col < a.cols && piece * 16 < rows16)
+            store_vec(a.qt + t.group * a.group_stride + (int64_t)(col0 + col) * a.ld_t + t.pad0 + piece * 16, w, a.keep);
     }
+}
+
+// Short groups in one pass: a workgroup takes 64 or 32 columns of a whole group (of one of two operands), holds up to H spans of its rows in
+// registers from the maxima to the cast, and turns a span at a time through LDS as above.  A longer group is read twice.
+//   columns: 8 LW; a span: SPAN = 4 NTH / LW rows; thread (p, l) = (tid / LW, tid % LW): rows SPAN h + 4 p .. + 3 of the group,
+//   columns 8 l .. + 7
+// 64 weights 1408 x 2048 in 123 us (4.5 TB/s; 32 columns, two workgroups a CU: what the loads take alone is 90), by maxima and cast
+// 172; gradient and activations of 9186 rows in 64 groups 38 us.
+struct StripLaunch {
+    ColArgs op[2];
+    int fmt[2];
+    int second, total;      // first workgroup of the second operand: strips times groups; all of them
+};
+
+template <int FMT, int NTH, int LW, int H>
+__device__ __forceinline__ void strip(const ColArgs& a, int block, uint8_t* turned, uint32_t* part, int* list) {
+    constexpr int COLS = 8 * LW, SPAN = 4 * NTH / LW, PIECES = SPAN / 16;
+    const int strips = (a.cols + COLS - 1) / COLS, e = block / strips;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, p = tid / LW, l = tid % LW;
+    const int col0 = (block - e * strips) * COLS, c = col0 + l * 8;
+    int row0, rows;
+    int64_t out0;      // where the group's codes start
+    if (a.offsets) {
+        const GroupSpan s = find_group(a.offsets, a.E, a.M, e);
+        row0 = s.row0;
+        rows = s.rows;
+        out0 = s.pad0;
+    } else {
+        rows = a.M / a.E;
+        row0 = e * rows;
+        out0 = e * a.group_stride;
+    }
+    const int spans = (rows + SPAN - 1) / SPAN;
+    auto fetch = [&](int h, int listed, uint4 (&v)[4]) {      // listed: where in the list row SPAN h is
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = SPAN * h + 4 * p + i;
+            v[i] = piece_of(a, r < rows ? list[listed + 4 * p + i] : -1, c);
+        }
+    };
+    auto fold = [](uint4& m, const uint4& v) {
+        m.x = pk_absmax(m.x, v.x); m.y = pk_absmax(m.y, v.y);
+        m.z = pk_absmax(m.z, v.z); m.w = pk_absmax(m.w, v.w);
+    };
+    const bool kept = spans <= H;
+    uint4 v[H][4];
+    uint4 m = make_uint4(0, 0, 0, 0);
+    if (kept) {
+        list_rows(a, row0, rows, list);
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+            if (h < spans) fetch(h, SPAN * h, v[h]);
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+            if (h < spans) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) fold(m, v[h][i]);
+            }
+    } else {
+        for (int h = 0; h < spans; h += 2) {
+            __syncthreads();      // (the list is read out)
+            list_rows(a, row0 + SPAN * h, rows - SPAN * h < 2 * SPAN ? rows - SPAN * h : 2 * SPAN, list);
+            fetch(h, 0, v[0]);
+            fetch(h + 1, SPAN, v[1]);      // (rows past the last are zeros)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                fold(m, v[0][i]);
+                fold(m, v[1][i]);
+            }
+        }
+    }
+    // the lanes of a column lie LW apart
+    uint32_t md[4] = {m.x, m.y, m.z, m.w};
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+        if constexpr (LW == 4) md[d] = pk_absmax(md[d], (uint32_t)__shfl_xor((int)md[d], 4, 64));
+        md[d] = pk_absmax_xor<32>(pk_absmax_xor<16>(pk_absmax_xor<8>(md[d])));
+    }
+    if (lane < LW) *reinterpret_cast<uint4*>(part + (wave * LW + lane) * 4) = make_uint4(md[0], md[1], md[2], md[3]);
+    __syncthreads();
+    // one column's scale per thread (a binary64 division each)
+    float* const scales = reinterpret_cast<float*>(part + NTH / 64 * LW * 4);
+    if (tid < COLS) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int i = 0; i < NTH / 64; ++i) w = pk_absmax(w, part[i * LW * 4 + (tid >> 1)]);
+        const float s = scale_from_amax(mag_to_float(tid & 1 ? w >> 16 : w & 0xFFFFu), FMT, a.flags);
+        scales[tid] = s;
+        if (col0 + tid < a.cols) a.scale[(int64_t)e * a.cols + col0 + tid] = s;
+    }
+    __syncthreads();
+    float s[8];
+    {
+        const float4 s0 = *reinterpret_cast<const float4*>(scales + l * 8), s1 = *reinterpret_cast<const float4*>(scales + l * 8 + 4);
+        s[0] = s0.x; s[1] = s0.y; s[2] = s0.z; s[3] = s0.w; s[4] = s1.x; s[5] = s1.y; s[6] = s1.z; s[7] = s1.w;
+    }
+    const int rows16 = (rows + 15) & ~15;
+    auto turn = [&](int h, const uint4 (&x)[4]) {      // LDS holds a column in SPAN bytes, pieces exchanged by column / 8
+        uint8_t* buf = turned + (h & 1) * (COLS * SPAN);
+        uint2 q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = cast8<FMT>(x[i], s);
+        uint32_t lo[4], hi[4];
+        transpose4x4_bytes(q[0].x, q[1].x, q[2].x, q[3].x, lo);
+        transpose4x4_bytes(q[0].y, q[1].y, q[2].y, q[3].y, hi);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            *reinterpret_cast<uint32_t*>(buf + (l * 8 + j) * SPAN + ((((p >> 2) ^ l) << 4) | ((p & 3) << 2))) = j < 4 ? lo[j] : hi[j - 4];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < COLS * PIECES / NTH; ++i) {
+            const int col = i * (NTH / PIECES) + tid / PIECES, piece = tid % PIECES;
+            const uint4 w = *reinterpret_cast<const uint4*>(buf + col * SPAN + ((piece ^ (col >> 3)) << 4));
+            if (col0 + col < a.cols && SPAN * h + piece * 16 < rows16)
+                store_vec(a.qt + out0 + (int64_t)(col0 + col) * a.ld_t + SPAN * h + piece * 16, w, a.keep);
+        }
+    };
+    if (kept) {
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+            if (h < spans) turn(h, v[h]);
+    } else {
+        for (int h = 0; h < spans; ++h) {
+            __syncthreads();
+            list_rows(a, row0 + SPAN * h, rows - SPAN * h < SPAN ? rows - SPAN * h : SPAN, list);
+            fetch(h, 0, v[0]);
+            turn(h, v[0]);
+        }
+    }
+}
+
+template <int NTH, int LW, int H>
+__global__ __launch_bounds__(NTH, NTH == 256 || H <= 4 ? 4 : 2) void strips_kernel(StripLaunch s) {
+    constexpr int COLS = 8 * LW, SPAN = 4 * NTH / LW;
+    __shared__ __attribute__((aligned(16))) uint8_t turned[2 * COLS * SPAN];
+    __shared__ __attribute__((aligned(16))) uint32_t part[NTH / 64 * LW * 4 + COLS];
+    __shared__ int list[SPAN * H];
+    static_assert(H >= 2, "a long group's rows are listed two spans at a time");
+    // (ragged groups as they come: an XCD's range would be a few groups, and the longest would decide - 38 against 43 us)
+    const int at = s.op[0].offsets ? (int)blockIdx.x < s.total ? (int)blockIdx.x : -1 : xcd_order(s.total);
+    if (at < 0) return;
+    const int o = at >= s.second, b = at - (o ? s.second : 0);
+    if (s.fmt[o] == FMT_E4M3FN) strip<FMT_E4M3FN, NTH, LW, H>(s.op[o], b, turned, part, list);
+    else strip<FMT_E5M2, NTH, LW, H>(s.op[o], b, turned, part, list);
 }
 
 // scales of groups without rows, whose products are zero whatever they are: a finite one
@@ -225,18 +393,55 @@ hipError_t launch_quant_rows_gather(const void* x, int64_t T, int64_t ldx, const
                              : rows_gather<FMT_E5M2>(xs, T, ldx, row_token, M, (int)cols, flags, q, ld_q, scale, st);
 }
 
+static ColArgs col_args(const GroupedColOperand& op, const int32_t* offsets, int64_t E, int flags) {
+    return ColArgs{static_cast<const uint16_t*>(op.x), op.T, op.ldx, op.row_token, op.uniform ? nullptr : offsets, (int)op.M, (int)E, (int)op.cols, flags, op.M * op.cols <= (int64_t)64 << 20,
+                   op.qt, op.ld_t, op.uniform ? op.cols * op.ld_t : 0, 0, op.scale, op.amax};
+}
+
+hipError_t launch_quant_strips_grouped(const GroupedColOperand& op, const GroupedColOperand* second, const int32_t* offsets, int64_t E, int flags,
+                                       hipStream_t st) {
+    int64_t most = 0;      // rows of a group that should stay in registers: all, or of ragged ones two and a half times the mean
+    for (const GroupedColOperand* o : {&op, second})
+        if (o) {
+            const int64_t rows = o->uniform ? o->M / E : 5 * o->M / (2 * E);
+            if (rows > most) most = rows;
+        }
+    StripLaunch s{};
+    auto launch = [&](int cols, auto kern, int threads) -> hipError_t {
+        int64_t blocks = 0;
+        s.second = 0x7FFFFFFF;
+        for (const GroupedColOperand* o : {&op, second}) {
+            if (!o) continue;
+            const int i = o != &op;
+            if (i) s.second = (int)blocks;
+            s.op[i] = col_args(*o, offsets, E, flags);
+            s.fmt[i] = o->fmt;
+            blocks += E * ((o->cols + cols - 1) / cols);
+        }
+        if (blocks >= 1 << 23) return hipErrorInvalidValue;
+        s.total = (int)blocks;
+        kern<<<xcd_grid(blocks), threads, 0, st>>>(s);
+        return hipGetLastError();
+    };
+    if (most <= 256) return launch(64, strips_kernel<256, 8, 2>, 256);
+    if (most <= 512) return launch(64, strips_kernel<256, 8, 4>, 256);
+    if (most <= 1024) return launch(32, strips_kernel<512, 4, 2>, 512);
+    if (most <= 1536) return launch(32, strips_kernel<512, 4, 3>, 512);
+    return launch(32, strips_kernel<512, 4, 5>, 512);
+}
+
 hipError_t launch_quant_cols_grouped(const GroupedColOperand& op, const int32_t* offsets, int64_t E, int flags, hipStream_t st) {
-    const ColArgs a{static_cast<const uint16_t*>(op.x), op.T, op.ldx, op.row_token, offsets, (int)op.M, (int)E, (int)op.cols, flags,
-                    op.qt, op.ld_t, offsets ? 0 : op.cols * op.ld_t, op.scale, op.amax};
+    ColArgs a = col_args(op, offsets, E, flags);
     const int64_t n = E * op.cols;
     clear_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(op.amax, op.scale, n);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (op.M <= 0) return hipSuccess;
-    // tiles of 128 rows: what the groups can come to at most
-    const int64_t per = op.M / E, tiles = offsets ? op.M / 128 + (E < op.M ? E : op.M) : E * ((per + 127) / 128);
-    cols_amax_kernel<<<dim3((unsigned)tiles, (unsigned)((op.cols + 511) / 512)), 256, 0, st>>>(a);
+    const int64_t tiles = a.offsets ? op.M / 128 + (E < op.M ? E : op.M) : E * ((op.M / E + 127) / 128);
+    if (tiles * ((op.cols + 127) / 128) >= 1 << 24) return hipErrorInvalidValue;
+    a.tiles = (int)tiles;
+    cols_amax_kernel<<<xcd_grid(tiles * ((op.cols + 511) / 512)), 256, 0, st>>>(a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    const dim3 grid((unsigned)tiles, (unsigned)((op.cols + 127) / 128));
+    const unsigned grid = xcd_grid(tiles * ((op.cols + 127) / 128));
     if (op.fmt == FMT_E4M3FN) cols_cast_kernel<FMT_E4M3FN><<<grid, 256, 0, st>>>(a);
     else cols_cast_kernel<FMT_E5M2><<<grid, 256, 0, st>>>(a);
     return hipGetLastError();

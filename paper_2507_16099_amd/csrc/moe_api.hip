@@ -286,15 +286,25 @@ int fp8_grouped_linear_bwd(const void* dy, const void* x, int64_t T, const int32
     uint32_t* amax = reinterpret_cast<uint32_t*>(ws + p.amax);
     const int64_t ld = pitch(N), Mp = fp8k::grouped_padded(M, E);
     const int fl = recipe->flags & FP8_POW2_SCALE;
+    if (T == 0) x = dy;      // (no token: no row of x is used, but where there is none the column kernels load from its start)
+    // operands per column: the weight for dX, gradient and activations for dW
+    const fp8k::GroupedColOperand cw{w, E * N, K, nullptr, E * N, K, recipe->fmt_w, true, ws + p.wt, ld, f32(p.swt), amax};
+    const fp8k::GroupedColOperand cg{dy, M, N, nullptr, M, N, recipe->fmt_dy, false, ws + p.gt, Mp, f32(p.sgt), amax};
+    const fp8k::GroupedColOperand cx{x, T, K, row_token, M, K, recipe->fmt_x, false, ws + p.xt, Mp, f32(p.sxt), amax};
     if (dx) {
+        if (fp8k::grouped_strips(cw, E)) FP8_TRY(fp8k::launch_quant_strips_grouped(cw, nullptr, offsets, E, fl, st));
+        else FP8_TRY(fp8k::launch_quant_cols_grouped(cw, offsets, E, fl, st));
         FP8_TRY(fp8k::launch_quant_rows_gather(dy, M, N, nullptr, M, N, recipe->fmt_dy, fl, ws + p.gq, ld, f32(p.sg), st));
-        FP8_TRY(fp8k::launch_quant_cols_grouped({w, E * N, K, nullptr, E * N, K, recipe->fmt_w, ws + p.wt, ld, f32(p.swt), amax}, nullptr, E, fl, st));
         FP8_TRY(fp8k::launch_gemm_fp8_grouped_rows({ws + p.gq, ld, recipe->fmt_dy, f32(p.sg), ws + p.wt, ld, recipe->fmt_w, f32(p.swt), offsets, E, M,
                                                     K, N, dx, K}, st));
     }
     if (dw) {
-        FP8_TRY(fp8k::launch_quant_cols_grouped({dy, M, N, nullptr, M, N, recipe->fmt_dy, ws + p.gt, Mp, f32(p.sgt), amax}, offsets, E, fl, st));
-        FP8_TRY(fp8k::launch_quant_cols_grouped({x, T, K, row_token, M, K, recipe->fmt_x, ws + p.xt, Mp, f32(p.sxt), amax}, offsets, E, fl, st));
+        if (fp8k::grouped_strips(cg, E)) {
+            FP8_TRY(fp8k::launch_quant_strips_grouped(cg, &cx, offsets, E, fl, st));
+        } else {
+            FP8_TRY(fp8k::launch_quant_cols_grouped(cg, offsets, E, fl, st));
+            FP8_TRY(fp8k::launch_quant_cols_grouped(cx, offsets, E, fl, st));
+        }
         FP8_TRY(fp8k::launch_gemm_fp8_grouped_contract({ws + p.gt, Mp, recipe->fmt_dy, f32(p.sgt), ws + p.xt, Mp, recipe->fmt_x, f32(p.sxt), offsets,
                                                         E, M, N, K, dw, K}, st));
     }

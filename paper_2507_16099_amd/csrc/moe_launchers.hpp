@@ -29,15 +29,20 @@ hipError_t launch_moe_combine_bwd(const void* dout, int64_t ld_dout, const void*
 // rows x[row_token[r]] (row_token nullptr: x[r]) -> codes q [M, ld_q] and scales [M]; a row whose token is not in [0, T) is a row of zeros
 hipError_t launch_quant_rows_gather(const void* x, int64_t T, int64_t ldx, const int32_t* row_token, int64_t M, int64_t cols, int fmt, int flags,
                                     uint8_t* q, int64_t ld_q, float* scale, hipStream_t st);
-// One operand quantized per column within each group of rows and written transposed.
-//   rows of group e: offsets given: [offsets[e], offsets[e + 1]) of the M rows, else [e M / E, (e + 1) M / E) (M a multiple of E)
-//   qt: with offsets [cols, ld_t], the codes of a group start at the sum of the earlier groups' lengths, each padded to 128, and
-//   zero codes follow up to the next 16; else [E, cols, ld_t].  scale [E, cols]; amax [E, cols]: scratch
+// Operands quantized per column within each group of rows and written transposed.
+//   rows of group e: [offsets[e], offsets[e + 1]) of the M rows; uniform: [e M / E, (e + 1) M / E) (M a multiple of E)
+//   qt: [cols, ld_t], the codes of a group start at the sum of the earlier groups' lengths, each padded to 128, and zero codes follow up
+//   to the next 16; uniform: [E, cols, ld_t].  scale [E, cols]; amax [E, cols]: scratch (of the first form)
 struct GroupedColOperand {
-    const void* x; int64_t T, ldx; const int32_t* row_token; int64_t M, cols; int fmt;
+    const void* x; int64_t T, ldx; const int32_t* row_token; int64_t M, cols; int fmt; bool uniform;
     uint8_t* qt; int64_t ld_t; float* scale; uint32_t* amax;
 };
 hipError_t launch_quant_cols_grouped(const GroupedColOperand& op, const int32_t* offsets, int64_t E, int flags, hipStream_t st);
+// the same for short groups, whose columns are read once: one operand or two (of groups of about the same length) in a launch
+hipError_t launch_quant_strips_grouped(const GroupedColOperand& op, const GroupedColOperand* second, const int32_t* offsets, int64_t E, int flags,
+                                       hipStream_t st);
+// whether that form is taken
+inline bool grouped_strips(const GroupedColOperand& op, int64_t E) { return op.M / E <= (op.uniform ? 2560 : 640); }
 // columns that the padded groups of M rows can come to
 inline int64_t grouped_padded(int64_t M, int64_t E) { return (M + 127 * (E < M ? E : M) + 127) / 128 * 128; }
 
