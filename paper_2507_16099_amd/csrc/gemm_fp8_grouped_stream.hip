@@ -5,7 +5,8 @@
 // What is different: the tiles.  A workgroup first reads the offsets and leaves in LDS, behind the stages, where each group's rows
 // start and how many tiles the groups before it have; the tile list is then walked like that of one product.
 //   rows      a tile's rows end with its group; the rows behind the last group are tiles without codes, which come out as zeros
-//   contract  the length of the contraction is the group's: at least four K steps are walked, those past its end fetch zeros
+//   contract  the length of the contraction is the group's.  A tile of up to 256 rows is one pair of K steps, which drains the tile
+//             before it in its first and itself from its second step on; so a tile's scales are requested a tile ahead.
 // (A lookup is a few LDS reads per tile, between two K steps.)
 // Tiles are dealt in rounds: the eight XCDs work on neighbouring runs of the tile order at any time, so that every round has tiles of
 // about the same group and all workgroups contract about the same length.  An XCD's own contiguous range of all tiles, as in the
@@ -20,6 +21,7 @@ namespace fp8k {
 
 namespace {
 
+enum { ST_ONLY = 4 };      // a pair that is a tile's first and last
 constexpr int TABLE_GROUPS = (160 * 1024 - st::LDS_BYTES) / 12 - 2;      // what the LDS has left holds three numbers per group
 
 struct GroupedStreamArgs {
@@ -40,7 +42,8 @@ struct GroupedTile {
     int valid;
 };
 
-template <int FA, int FB, int AF1, bool CONTRACT>
+// SHORT: tiles of short groups take one pair of K steps (192-row tiles only: with it the 256-row ones spill fragments)
+template <int FA, int FB, int AF1, bool CONTRACT, bool SHORT = false>
 __global__ __launch_bounds__(st::NT) void gemm_fp8_grouped_stream_kernel(GroupedStreamArgs p) {
     using namespace st;
     static_assert(AF1 >= 2 && AF1 <= 4, "the A1 group has two to four fragments");
@@ -301,10 +304,11 @@ __global__ __launch_bounds__(st::NT) void gemm_fp8_grouped_stream_kernel(Grouped
         }(std::make_integer_sequence<int, 16>{});
     };
 
-    // pairs of K steps of a tile: two at least, an odd count of steps gets one of zeros
-    auto kpairs_of = [&](const GroupedTile& t) {
-        const int pairs = ((t.k + BK - 1) / BK + 1) / 2;
-        return pairs < 2 ? 2 : pairs;
+    // pairs of K steps of a tile (an odd count of steps gets one of zeros): two at least, with SHORT one, except for a workgroup's
+    // first tile, in front of which there is nothing to drain
+    auto kpairs_of = [&](const GroupedTile& t, int j) {
+        const int pairs = ((t.k + BK - 1) / BK + 1) / 2, least = SHORT && j > 0 ? 1 : 2;
+        return pairs < least ? least : pairs;
     };
 
     // reciprocal scales of a tile, one row and one column per thread (correctly rounded divides).  The raw scales come into
@@ -338,13 +342,13 @@ __global__ __launch_bounds__(st::NT) void gemm_fp8_grouped_stream_kernel(Grouped
     };
 
     // a pair of K steps (the B halves swap roles every step).  KIND: ST_FIRST(_DRAIN) = steps 0, 1 of a tile (step 0
-    // starts the accumulators from zero; with _DRAIN the rest of the previous tile leaves in its phases 1-3; the scale
-    // loads of this tile go out in step 0, its table is written in step 1), ST_MIDDLE, ST_LAST = the last two steps
+    // starts the accumulators from zero; with _DRAIN the rest of the previous tile leaves in its phases 1-3; this tile's table of
+    // reciprocal scales is written in step 0), ST_MIDDLE, ST_LAST = the last two steps, ST_ONLY = both (the last steps also request the next tile's scales
     // (refills fetch steps 0, 1 of tile `lt` = the next tile; the drain of this tile starts in phase 2 of the last step).
-    auto pair = [&](auto kind_t, const GroupedTile& cur, const GroupedTile& lt, int k2_even, const Drain& dprev, const Drain& dcur, float* tab_cur) {
+    auto pair = [&](auto kind_t, const GroupedTile& cur, const GroupedTile& lt, int k2_even, const Drain& dprev, const Drain& dcur, float* tab_cur, float* tab_nxt) {
         constexpr int KIND = decltype(kind_t)::value;
-        constexpr bool FIRST = KIND == ST_FIRST || KIND == ST_FIRST_DRAIN;
-        constexpr bool FD = KIND == ST_FIRST_DRAIN, LD = KIND == ST_LAST;
+        constexpr bool FIRST = KIND == ST_FIRST || KIND == ST_FIRST_DRAIN || KIND == ST_ONLY;
+        constexpr bool FD = KIND == ST_FIRST_DRAIN || KIND == ST_ONLY, LD = KIND == ST_LAST || KIND == ST_ONLY;
         using Z = std::integral_constant<int, FIRST ? 1 : 0>;
         using NJ = StNoJobs;
         {
@@ -357,7 +361,7 @@ __global__ __launch_bounds__(st::NT) void gemm_fp8_grouped_stream_kernel(Grouped
             st_barrier_lds();                  // this step's B part is read out by everyone
             phase(I0{}, I1{}, I1{}, I1{}, I0{}, I5{}, Z{}, std::conditional_t<FD, StJobsF2, NJ>{}, s_cur, la, lb, lt, ko, dprev);   // (A0,B1) | read A1 of this step, refill B 0-4
             st_wait_vmem_but_barrier<5 + (FD ? st_extra_f(AF1) : 0)>();   // step k+1 has landed for everyone; this step's A part is read out
-            if constexpr (FIRST) scale_loads(cur, tab_cur);   // older than the refill loads below: complete at the next such wait
+            if constexpr (FIRST) scale_table(cur, tab_cur);   // (its loads: the last step of the tile before)
             phase(I1{}, I1{}, I1{}, I0{}, I5{}, I6{}, Z{}, std::conditional_t<FD, StJobsF3, NJ>{}, s_nxt, la, lb, lt, ko, dprev);   // (A1,B1) | read A0 of step k+1, refill B 5-7, A 0-2
             phase(I1{}, I0{}, I0{}, I1{}, I11{}, I5{}, Z{}, NJ{}, s_nxt, la, lb, lt, ko, dprev);                                    // (A1,B0) | read B1 of step k+1, refill A 3-7
         }
@@ -371,7 +375,7 @@ __global__ __launch_bounds__(st::NT) void gemm_fp8_grouped_stream_kernel(Grouped
             st_barrier_lds();
             phase(I0{}, I0{}, I1{}, I1{}, I0{}, I5{}, I0{}, std::conditional_t<LD, StJobsL2, NJ>{}, s_cur, la, lb, lt, ko, dcur);   // (A0,B0) | read A1 of this step, refill B 0-4
             st_wait_vmem_but_barrier<5 + (LD ? st_extra_l(AF1) : 0)>();
-            if constexpr (FIRST) scale_table(cur, tab_cur);
+            if constexpr (LD) scale_loads(lt, tab_nxt);   // older than the refill loads below: complete at the next such wait
             phase(I1{}, I0{}, I1{}, I0{}, I5{}, I6{}, I0{}, std::conditional_t<LD, StJobsL3, NJ>{}, s_nxt, la, lb, lt, ko, dcur);   // (A1,B0) | read A0 of step k+1, refill B 5-7, A 0-2
             phase(I1{}, I1{}, I0{}, I0{}, I11{}, I5{}, I0{}, std::conditional_t<LD, StJobsL4, NJ>{}, s_nxt, la, lb, lt, ko, dcur);  // (A1,B1) | read B0 of step k+1, refill A 3-7
         }
@@ -381,6 +385,7 @@ __global__ __launch_bounds__(st::NT) void gemm_fp8_grouped_stream_kernel(Grouped
     GroupedTile cur = tile_of(0);
     issue_loads(cur, 0, 0);
     issue_loads(cur, 1, BK);
+    scale_loads(cur, tab0);
     st_wait_all_vmem();
     __syncthreads();
 #pragma unroll
@@ -393,20 +398,30 @@ __global__ __launch_bounds__(st::NT) void gemm_fp8_grouped_stream_kernel(Grouped
     GroupedTile prev = cur;
     for (int j = 0; j < my_tiles; ++j) {
         float* tab_cur = tab0 + (j & 1) * (TAB / 4);
-        const int kpairs = kpairs_of(cur);
-        {
-            const Drain dprev = drain_of(prev, j - 1);
-            if (j == 0) pair(std::integral_constant<int, ST_FIRST>{}, cur, cur, 2 * BK, dprev, dprev, tab_cur);
-            else pair(std::integral_constant<int, ST_FIRST_DRAIN>{}, cur, cur, 2 * BK, dprev, dprev, tab_cur);
+        float* tab_nxt = tab0 + (~j & 1) * (TAB / 4);
+        const int kpairs = kpairs_of(cur, j);
+        GroupedTile nxt;
+        bool done = false;
+        if constexpr (SHORT) {
+            if (kpairs == 1) {
+                nxt = tile_of(j + 1);
+                pair(std::integral_constant<int, ST_ONLY>{}, cur, nxt, 0, drain_of(prev, j - 1), drain_of(cur, j), tab_cur, tab_nxt);
+                done = true;
+            }
         }
-        for (int kp = 1; kp < kpairs - 1; ++kp) {
-            const Drain none = drain_of(cur, j);
-            pair(std::integral_constant<int, ST_MIDDLE>{}, cur, cur, (2 * kp + 2) * BK, none, none, tab_cur);
-        }
-        const GroupedTile nxt = tile_of(j + 1);
-        {
+        if (!done) {
+            {
+                const Drain dprev = drain_of(prev, j - 1);
+                if (j == 0) pair(std::integral_constant<int, ST_FIRST>{}, cur, cur, 2 * BK, dprev, dprev, tab_cur, tab_nxt);
+                else pair(std::integral_constant<int, ST_FIRST_DRAIN>{}, cur, cur, 2 * BK, dprev, dprev, tab_cur, tab_nxt);
+            }
+            for (int kp = 1; kp < kpairs - 1; ++kp) {
+                const Drain none = drain_of(cur, j);
+                pair(std::integral_constant<int, ST_MIDDLE>{}, cur, cur, (2 * kp + 2) * BK, none, none, tab_cur, tab_nxt);
+            }
+            nxt = tile_of(j + 1);
             const Drain dcur = drain_of(cur, j);
-            pair(std::integral_constant<int, ST_LAST>{}, cur, nxt, 0, dcur, dcur, tab_cur);
+            pair(std::integral_constant<int, ST_LAST>{}, cur, nxt, 0, dcur, dcur, tab_cur, tab_nxt);
         }
         prev = cur;
         cur = nxt;
@@ -424,11 +439,11 @@ __global__ __launch_bounds__(st::NT) void gemm_fp8_grouped_stream_kernel(Grouped
     }
 }
 
-template <int FA, int FB, int AF1, bool CONTRACT>
+template <int FA, int FB, int AF1, bool CONTRACT, bool SHORT = false>
 hipError_t launch_t(const GroupedGemm& g, hipStream_t st) {
     using namespace st;
     constexpr int TM = 32 * (4 + AF1);
-    auto kern = gemm_fp8_grouped_stream_kernel<FA, FB, AF1, CONTRACT>;
+    auto kern = gemm_fp8_grouped_stream_kernel<FA, FB, AF1, CONTRACT, SHORT>;
     static DynamicLdsOnce attr;
     if (hipError_t e = attr.ensure(reinterpret_cast<const void*>(kern), 160 * 1024); e != hipSuccess) return e;
     int64_t cus = compute_units();
@@ -449,6 +464,7 @@ template <int FA, int FB>
 hipError_t launch_rows(const GroupedGemm& g, hipStream_t st) { return launch_t<FA, FB, 4, false>(g, st); }
 template <int FA, int FB>
 hipError_t launch_contract(const GroupedGemm& g, hipStream_t st) {
+    if (g.M <= 192 * g.E) return launch_t<FA, FB, 2, true, true>(g, st);
     const int64_t rows = gemm_fp8_stream_tile_m(g.N * g.E, g.K);
     return rows == 256 ? launch_t<FA, FB, 4, true>(g, st) : rows == 224 ? launch_t<FA, FB, 3, true>(g, st) : launch_t<FA, FB, 2, true>(g, st);
 }

@@ -425,6 +425,8 @@ hipError_t launch_quant_strips_grouped(const GroupedColOperand& op, const Groupe
     };
     if (most <= 256) return launch(64, strips_kernel<256, 8, 2>, 256);
     if (most <= 512) return launch(64, strips_kernel<256, 8, 4>, 256);
+    if (!(op.uniform && (!second || second->uniform)))
+        return most <= 1024 ? launch(64, strips_kernel<512, 8, 4>, 512) : launch(64, strips_kernel<512, 8, 6>, 512);
     if (most <= 1024) return launch(32, strips_kernel<512, 4, 2>, 512);
     if (most <= 1536) return launch(32, strips_kernel<512, 4, 3>, 512);
     return launch(32, strips_kernel<512, 4, 5>, 512);
