@@ -14,6 +14,9 @@
 #include "group_tiles.hpp"
 #include "moe_launchers.hpp"
 
+#include <algorithm>
+#include <cmath>
+
 namespace fp8k {
 
 namespace {
@@ -121,9 +124,9 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void gemm_fp8_grouped_kerne
             else if (u < NU) lds_dma4(rsrc_sb, at, (uint32_t)(r < rows_b ? r : rows_b - 1) * 4u);
         }
     }
-    auto scale_table = [&]() {       // (a tile without K steps is zero whatever stands in its rows' scales)
+    auto scale_table = [&]() {       // (a tile without K steps is zero whatever stands in its scales)
         if (tid < TM) inv_tab[tid] = Kt ? 1.0f / inv_tab[tid] : 0.0f;
-        if (tid < TN) inv_tab[TMS + tid] = 1.0f / inv_tab[TMS + tid];
+        if (tid < TN) inv_tab[TMS + tid] = Kt ? 1.0f / inv_tab[TMS + tid] : 0.0f;
     };
 
     const int lrow = lane >> 3;
@@ -300,29 +303,56 @@ hipError_t launch_t(const GroupedGemm& g, hipStream_t st) {
     return hipGetLastError();
 }
 
-// the tile forms (of RingTile, launchers.hpp): height, width, stages, tile rows walked together
-template <int FA, int FB, bool CONTRACT>
-hipError_t launch_tile(int tile, const GroupedGemm& g, hipStream_t st) {
-    switch (tile) {
-        case RING_64x64: return launch_t<FA, FB, 64, 64, 2, 2, 4, 4, CONTRACT>(g, st);
-        case RING_128x64: return launch_t<FA, FB, 128, 64, 2, 2, 3, 4, CONTRACT>(g, st);
-        case RING_64x128: return launch_t<FA, FB, 64, 128, 2, 2, 4, 8, CONTRACT>(g, st);
-        case RING_128x256: return launch_t<FA, FB, 128, 256, 2, 2, 3, 8, CONTRACT>(g, st);
-        case RING_96x128: return launch_t<FA, FB, 96, 128, 2, 2, 4, 8, CONTRACT>(g, st);
-        case RING_192x128: return launch_t<FA, FB, 192, 128, 2, 2, 3, 4, CONTRACT>(g, st);
-        case RING_256x128: return launch_t<FA, FB, 256, 128, 2, 2, 3, 4, CONTRACT>(g, st);
-        default: return launch_t<FA, FB, 128, 128, 2, 2, 4, 4, CONTRACT>(g, st);
+// The tile forms: those of RingTile (launchers.hpp) that pay here, one of 32 rows, and the persistent kernel's 256 x 256.
+enum Form { F_32x128 = 0, F_64x64, F_64x128, F_128x128, F_192x128, F_128x256, F_STREAM, FORMS };
+// What a form takes, in us: a K step of 128 and the rest of a tile, times the rounds of tiles on the CUs (64 x 64: two tiles a CU), and
+// the bytes at `rate`, whichever is more, as the fourth root of the sum of fourth powers (both count where they are close).  Fitted to 207
+// forwards of 26 shapes (4 .. 128 experts, K and N 512 .. 14400, 1/4 .. 4096 rows an expert on average, groups a factor of 8 apart): off by
+// 11 % in the root mean square, and the form with the least estimate is 5 % behind the best of ten forms on average, 36 % at worst; by
+// the mean number of rows alone (up to 16, 64, 256) 12 % and 86 %.  Others that were tried gain under 0.5 % together: 128 x 64, 96 x 128,
+// 256 x 128.
+struct FormCost { int tm, tn, tiles_per_cu; double step, tile; };
+constexpr FormCost kForms[FORMS] = {{32, 128, 1, 0.303, 3.9}, {64, 64, 2, 0.408, 2.9}, {64, 128, 1, 0.382, 3.2}, {128, 128, 1, 0.508, 3.8},
+                                    {192, 128, 1, 0.589, 4.7}, {128, 256, 1, 0.765, 5.6}, {256, 256, 1, 1.151, 7.2}};
+double form_cost(const FormCost& f, const GroupedGemm& g, int64_t cus) {
+    constexpr double rate = 5.1e6;      // bytes a us
+    const double busy = g.E < g.M ? (double)g.E : (double)g.M, mean = (double)g.M / (double)g.E;
+    // row tiles: groups that have rows have one, longer ones half a tile more than their rows fill
+    const double row_tiles = mean < 1 ? busy : busy * std::max(1.0, mean / f.tm + 0.5);
+    const double full = row_tiles * (double)((g.N + f.tn - 1) / f.tn) / (double)(cus * f.tiles_per_cu);
+    const double rounds = (std::ceil(0.9 * full) + std::ceil(full) + std::ceil(1.1 * full)) / 3;      // (the number of tiles is an estimate)
+    const double compute = rounds * ((double)((g.K + 127) / 128) * f.step + f.tile);
+    const double bytes = (busy * (double)g.K * (double)g.N + (double)g.M * (double)g.K + 2.0 * (double)g.M * (double)g.N) / rate;
+    return std::sqrt(std::sqrt(compute * compute * compute * compute + bytes * bytes * bytes * bytes));
+}
+
+template <int FA, int FB>
+hipError_t launch_form(int form, const GroupedGemm& g, hipStream_t st) {
+    switch (form) {
+        case F_64x64: return launch_t<FA, FB, 64, 64, 2, 2, 4, 4, false>(g, st);
+        case F_64x128: return launch_t<FA, FB, 64, 128, 2, 2, 4, 8, false>(g, st);
+        case F_192x128: return launch_t<FA, FB, 192, 128, 2, 2, 3, 4, false>(g, st);
+        case F_128x256: return launch_t<FA, FB, 128, 256, 2, 2, 3, 8, false>(g, st);
+        case F_32x128: return launch_t<FA, FB, 32, 128, 1, 4, 6, 1, false>(g, st);
+        default: return launch_t<FA, FB, 128, 128, 2, 2, 4, 4, false>(g, st);
     }
 }
 
 template <int FA, int FB>
 hipError_t launch_rows(const GroupedGemm& g, hipStream_t st) {
-    const int64_t mean = g.M / g.E;
-    const int ring = knob(KNOB_GEMM_RING), stream = knob(KNOB_GEMM_STREAM);
-    if (ring > 0) return launch_tile<FA, FB, false>(ring - 1, g, st);
-    if ((stream >= 2 || (stream != 0 && mean >= 256)) && gemm_fp8_grouped_stream_fits(g)) return launch_gemm_fp8_grouped_stream_rows(g, st);
-    if (mean <= 16) return launch_t<FA, FB, 32, 128, 1, 4, 6, 1, false>(g, st);
-    return launch_tile<FA, FB, false>(mean <= 64 ? RING_64x128 : RING_128x128, g, st);
+    const int forced = knob(KNOB_GEMM_RING), stream = knob(KNOB_GEMM_STREAM);      // 1 + form; 0: never, 2: wherever it fits
+    int form = 0;
+    if (forced > 0) {
+        form = forced - 1 < F_STREAM ? forced - 1 : F_128x128;
+    } else {
+        const int64_t cus = compute_units() > 0 ? compute_units() : 256;
+        const bool fits = stream != 0 && gemm_fp8_grouped_stream_fits(g);
+        for (int f = 1; f < (fits ? FORMS : F_STREAM); ++f)
+            if (form_cost(kForms[f], g, cus) < form_cost(kForms[form], g, cus)) form = f;
+        if (fits && stream >= 2) form = F_STREAM;
+    }
+    if (form == F_STREAM) return launch_gemm_fp8_grouped_stream_rows(g, st);
+    return launch_form<FA, FB>(form, g, st);
 }
 
 }  // namespace
@@ -338,12 +368,12 @@ hipError_t launch_gemm_fp8_grouped_rows(const GroupedGemm& g, hipStream_t st) {
     FP8K_FORMATS(launch_rows)
 }
 
+// dW: the persistent kernel (64 experts 1408 x 2048 of 16 .. 2048 rows: 86 to 430 us, 128 x 256 tiles 150 to 620), tiles for the
+// tables of groups that its LDS has no room for
 template <int FA, int FB>
 static hipError_t launch_contract(const GroupedGemm& g, hipStream_t st) {
-    const int ring = knob(KNOB_GEMM_RING);
-    if (ring > 0) return launch_tile<FA, FB, true>(ring - 1, g, st);
     if (knob(KNOB_GEMM_STREAM) != 0 && gemm_fp8_grouped_stream_fits(g)) return launch_gemm_fp8_grouped_stream_contract(g, st);
-    return launch_tile<FA, FB, true>(RING_128x128, g, st);
+    return launch_t<FA, FB, 128, 128, 2, 2, 4, 4, true>(g, st);
 }
 hipError_t launch_gemm_fp8_grouped_contract(const GroupedGemm& g, hipStream_t st) { FP8K_FORMATS(launch_contract) }
 

@@ -154,37 +154,16 @@ __global__ __launch_bounds__(64 * WAVES) void grouped_few_kernel(FewArgs p) {
             const uint4 v = *reinterpret_cast<const uint4*>(real ? row + k : p.x);
             return make_uint4(real ? v.x : 0u, real ? v.y : 0u, real ? v.z : 0u, real ? v.w : 0u);
         };
-        // (without these the compiler requests all pieces of a long row at once, and spills)
-        auto every_fourth = [&](int s) {
-            if (s % 4 == 3) {
-                asm volatile("" ::: "memory");
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        };
-        constexpr bool KEEP = PER <= 4;       // else the rows are read again for the cast (they are in the caches then)
-        uint4 kept[KEEP ? PER : 1][4];
+        uint4 v[PER][4];
         uint32_t m = 0;
 #pragma unroll
-        for (int s = 0; s < PER; ++s) {
-            uint4 v[4];
+        for (int s = 0; s < PER; ++s)
 #pragma unroll
-            for (int h = 0; h < 4; ++h) v[h] = piece(s, h);
+            for (int h = 0; h < 4; ++h) v[s][h] = piece(s, h);
 #pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                if constexpr (KEEP) kept[s][h] = v[h];
-                else m = pk_absmax4(m, v[h]);
-            }
-            if constexpr (!KEEP) {
-                asm volatile("" : "+v"(m));
-                every_fourth(s);
-            }
-        }
-        if constexpr (KEEP) {
+        for (int s = 0; s < PER; ++s)
 #pragma unroll
-            for (int s = 0; s < PER; ++s)
-#pragma unroll
-                for (int h = 0; h < 4; ++h) m = pk_absmax4(m, kept[s][h]);
-        }
+            for (int h = 0; h < 4; ++h) m = pk_absmax4(m, v[s][h]);
         m = pk_absmax_xor<32>(pk_absmax_xor<16>(m));
         if (g == 0) amax[wave * 16 + i] = pk_fold(m);
         barrier_lds();
@@ -197,12 +176,8 @@ __global__ __launch_bounds__(64 * WAVES) void grouped_few_kernel(FewArgs p) {
         for (int st = 0; st < PER; ++st) {
             uint2 q[4];
 #pragma unroll
-            for (int h = 0; h < 4; ++h) q[h] = cast8<FA>(KEEP ? kept[KEEP ? st : 0][h] : piece(st, h), s);
+            for (int h = 0; h < 4; ++h) q[h] = cast8<FA>(v[st][h], s);
             af[st] = v8i_g{(int)q[0].x, (int)q[0].y, (int)q[1].x, (int)q[1].y, (int)q[2].x, (int)q[2].y, (int)q[3].x, (int)q[3].y};
-            if constexpr (!KEEP) {
-                asm volatile("" : "+v"(af[st]));
-                every_fourth(st);
-            }
         }
     };
 
@@ -265,10 +240,21 @@ hipError_t launch_t(const FewArgs& a, int64_t grid, hipStream_t st) {
 
 }  // namespace
 
+// Where this form is taken, against quantization and tiles in two launches (us, the other / this, 8 experts 14336 x 4096 with 2, 4, 8, 16
+// rows in all 31.8 28.7 70.3 87.2 / 26.0 26.4 52.7 95.9; 64 experts 1408 x 2048, 2, 8, 32, 64, 128, 256, 512 rows 8.7 9.6 20.0 22.2
+// 35.6 40.9 42.2 / 8.4 13.2 20.7 22.1 30.0 34.3 44.8): up to six rows an expert on average, and one where the weights are large; a K
+// that the eight wavefronts share evenly (2048 x 1408, 64 rows, 21.0 / 35.7; longer ones than 4096, whose rows do not stay in registers
+// between maximum and cast: 4096 x 7168, 2 and 8 rows, 16.8 35.5 / 22.3 46.8); and weights enough that the stream decides.
+static bool few_rows_pay(const GroupedGemm& g) {
+    const double busy = (double)(g.E < g.M ? g.E : g.M);
+    const int64_t steps = (g.K + 127) / 128;
+    return g.M <= 6 * g.E && steps % WAVES == 0 && busy * (double)g.N * (double)g.K >= 64e6 && (g.M <= g.E || g.N * g.K <= (int64_t)16 << 20);
+}
+
 // hipErrorNotSupported (nothing launched): more rows, or a longer contraction, than it is for
 hipError_t launch_grouped_few(const void* x, int64_t T, const int32_t* row_token, int fmt_x, int flags, const GroupedGemm& g, hipStream_t st) {
-    const int forced = knob(KNOB_SKINNY_DMA);      // 0: never, 2: whatever the number of rows
-    if (forced == 0 || (g.M > 16 * g.E && forced < 2) || g.K > 16384 || T < 1) return hipErrorNotSupported;
+    const int forced = knob(KNOB_SKINNY_DMA);      // 0: never, 2: wherever it fits
+    if (forced == 0 || g.K > 4096 || T < 1 || (forced < 2 && !few_rows_pay(g))) return hipErrorNotSupported;
     const int64_t cus = compute_units() > 0 ? compute_units() : 256;
     const int64_t tiles_n = (g.N + 15) / 16, most = (g.M / 16 + (g.E + 1 < g.M ? g.E + 1 : g.M)) * tiles_n;
     if (most > 0x3FFFFFFF) return hipErrorNotSupported;
@@ -280,9 +266,7 @@ hipError_t launch_grouped_few(const void* x, int64_t T, const int32_t* row_token
 #define FP8K_FEW(FA_, FB_)                                                     \
     if (fmt_x == FA_ && g.fmt_b == FB_) {                                      \
         if (per <= 2) return launch_t<FA_, FB_, 2>(a, grid, st);               \
-        if (per <= 4) return launch_t<FA_, FB_, 4>(a, grid, st);               \
-        if (per <= 8) return launch_t<FA_, FB_, 8>(a, grid, st);               \
-        return launch_t<FA_, FB_, 16>(a, grid, st);                            \
+        return launch_t<FA_, FB_, 4>(a, grid, st);                             \
     }
     FP8K_FEW(FMT_E4M3FN, FMT_E4M3FN)
     FP8K_FEW(FMT_E5M2, FMT_E4M3FN)

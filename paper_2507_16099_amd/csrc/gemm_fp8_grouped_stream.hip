@@ -325,10 +325,10 @@ __global__ __launch_bounds__(st::NT) void gemm_fp8_grouped_stream_kernel(Grouped
     };
     auto scale_table = [&](const GroupedTile& t, float* tab) {
         // (the loads were issued ahead of a phase 3's refill loads and a wait that lets only younger operations stay in flight has
-        // passed; a tile without codes is zero whatever stands in its rows' scales)
+        // passed; a tile without codes is zero whatever stands in its scales)
         const float raw_a = tab[threadIdx.x], raw_b = tab[256 + threadIdx.x];
         tab[threadIdx.x] = t.k ? 1.0f / raw_a : 0.0f;
-        tab[256 + threadIdx.x] = 1.0f / raw_b;
+        tab[256 + threadIdx.x] = t.k ? 1.0f / raw_b : 0.0f;
     };
     float* const tab0 = reinterpret_cast<float*>(smem + 2 * STAGE);
 

@@ -33,6 +33,24 @@ __device__ __forceinline__ int wave_before(int v, int first) { return __builtin_
 // the value of one lane, the same lane for all
 __device__ __forceinline__ int at_lane(int v, int l) { return __builtin_amdgcn_readlane(v, __builtin_amdgcn_readfirstlane(l)); }
 
+// offsets[e + 1] of 64 groups at a time, requested four sixty-fours ahead (one behind the other, 256 groups are four trips to memory)
+struct OffsetChunks {
+    const int32_t* offsets;
+    int E, v[4];
+    __device__ __forceinline__ int at(int e) const { return offsets[(e < E ? e : E - 1) + 1]; }
+    __device__ __forceinline__ OffsetChunks(const int32_t* o, int E_) : offsets(o), E(E_) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = i * 64 < E ? at(i * 64 + (int)(threadIdx.x & 63)) : 0;
+    }
+    // of the groups from e0 on; called for e0 = 0, 64, 128, ...
+    __device__ __forceinline__ int get(int e0) {
+        const int r = v[0];
+        v[0] = v[1]; v[1] = v[2]; v[2] = v[3];
+        if (e0 + 256 < E) v[3] = at(e0 + 256 + (int)(threadIdx.x & 63));
+        return r;
+    }
+};
+
 struct GroupTile {
     int group;       // E: the rows behind the last group
     int row0, rows;  // of the tile
@@ -48,9 +66,11 @@ __device__ __forceinline__ GroupTile find_group_tile(const int32_t* __restrict__
     const int lane = threadIdx.x & 63;
     GroupTile t{-1, 0, 0, 0, 0, false};
     int end = 0, tiles_before = 0, pad_before = 0;
+    OffsetChunks chunks(offsets, E);
     for (int e0 = 0; e0 < E + (TAIL ? 1 : 0); e0 += 64) {
         const int e = e0 + lane;
-        int b = e < E ? offsets[e + 1] : TAIL && e == E ? M : 0;
+        int b = chunks.get(e0);
+        if (e >= E) b = TAIL && e == E ? M : 0;
         b = b < end ? end : b > M ? M : b;
         b = wave_scan_max(b);
         const int a = wave_before(b, end);
@@ -86,9 +106,11 @@ __device__ __forceinline__ GroupSpan find_group(const int32_t* __restrict__ offs
     const int lane = threadIdx.x & 63;
     GroupSpan s{0, 0, 0};
     int end = 0, pad_before = 0;
+    OffsetChunks chunks(offsets, E);
     for (int e0 = 0; e0 <= group; e0 += 64) {
         const int e = e0 + lane;
-        int b = e < E ? offsets[e + 1] : 0;
+        int b = chunks.get(e0);
+        if (e >= E) b = 0;
         b = b < end ? end : b > M ? M : b;
         b = wave_scan_max(b);
         const int a = wave_before(b, end);

@@ -124,6 +124,8 @@ __device__ __forceinline__ uint4 piece_of(const ColArgs& a, int row, int c) {
     return make_uint4(real ? v.x : 0u, real ? v.y : 0u, real ? v.z : 0u, real ? v.w : 0u);
 }
 
+// (A weight's experts one after the other, maxima and then cast, so that the cast finds them in the last-level cache: 428 us for eight of
+// 14336 x 4096, all maxima and then all casts 412.)
 // Maxima: a workgroup takes 512 columns (a lane eight) of up to HEIGHT rows of a group, a wavefront every fourth row.
 constexpr int AMAX_ROWS = 128;
 __global__ __launch_bounds__(256) void cols_amax_kernel(ColArgs a) {
@@ -374,15 +376,6 @@ __global__ __launch_bounds__(NTH, NTH == 256 || H <= 4 ? 4 : 2) void strips_kern
     else strip<FMT_E5M2, NTH, LW, H>(s.op[o], b, turned, part, list);
 }
 
-// scales of groups without rows, whose products are zero whatever they are: a finite one
-__global__ __launch_bounds__(256) void clear_kernel(uint32_t* __restrict__ amax, float* __restrict__ scale, int64_t n) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i < n) {
-        amax[i] = 0u;
-        scale[i] = 1.0f;
-    }
-}
-
 }  // namespace
 
 hipError_t launch_quant_rows_gather(const void* x, int64_t T, int64_t ldx, const int32_t* row_token, int64_t M, int64_t cols, int fmt, int flags,
@@ -433,11 +426,9 @@ hipError_t launch_quant_strips_grouped(const GroupedColOperand& op, const Groupe
 }
 
 hipError_t launch_quant_cols_grouped(const GroupedColOperand& op, const int32_t* offsets, int64_t E, int flags, hipStream_t st) {
-    ColArgs a = col_args(op, offsets, E, flags);
-    const int64_t n = E * op.cols;
-    clear_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(op.amax, op.scale, n);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (op.M <= 0) return hipSuccess;
+    ColArgs a = col_args(op, offsets, E, flags);
+    // tiles of 128 rows: what the groups can come to at most
     const int64_t tiles = a.offsets ? op.M / 128 + (E < op.M ? E : op.M) : E * ((op.M / E + 127) / 128);
     if (tiles * ((op.cols + 127) / 128) >= 1 << 24) return hipErrorInvalidValue;
     a.tiles = (int)tiles;

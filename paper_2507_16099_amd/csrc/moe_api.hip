@@ -96,7 +96,7 @@ BwdPlan plan_bwd(int64_t M, int64_t E, int64_t K, int64_t N) {
     p.sgt = take((size_t)E * N * 4);
     p.xt = take((size_t)K * Mp);                 // X codes [K, padded rows], scales [E, K]
     p.sxt = take((size_t)E * K * 4);
-    p.amax = take((size_t)E * (K > N ? K : N) * 4);
+    p.amax = take((size_t)E * (2 * K + N) * 4);  // largest magnitudes of W's, dY's and X's columns
     p.total = o;
     return p;
 }
@@ -283,23 +283,28 @@ int fp8_grouped_linear_bwd(const void* dy, const void* x, int64_t T, const int32
     FP8_CHECK(check_workspace(fn, workspace, workspace_bytes, p.total));
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     auto f32 = [&](size_t at) { return reinterpret_cast<float*>(ws + at); };
-    uint32_t* amax = reinterpret_cast<uint32_t*>(ws + p.amax);
+    uint32_t *amax_w = reinterpret_cast<uint32_t*>(ws + p.amax), *amax_g = amax_w + E * K, *amax_x = amax_g + E * N;
     const int64_t ld = pitch(N), Mp = fp8k::grouped_padded(M, E);
     const int fl = recipe->flags & FP8_POW2_SCALE;
     if (T == 0) x = dy;      // (no token: no row of x is used, but where there is none the column kernels load from its start)
     // operands per column: the weight for dX, gradient and activations for dW
-    const fp8k::GroupedColOperand cw{w, E * N, K, nullptr, E * N, K, recipe->fmt_w, true, ws + p.wt, ld, f32(p.swt), amax};
-    const fp8k::GroupedColOperand cg{dy, M, N, nullptr, M, N, recipe->fmt_dy, false, ws + p.gt, Mp, f32(p.sgt), amax};
-    const fp8k::GroupedColOperand cx{x, T, K, row_token, M, K, recipe->fmt_x, false, ws + p.xt, Mp, f32(p.sxt), amax};
+    const fp8k::GroupedColOperand cw{w, E * N, K, nullptr, E * N, K, recipe->fmt_w, true, ws + p.wt, ld, f32(p.swt), amax_w};
+    const fp8k::GroupedColOperand cg{dy, M, N, nullptr, M, N, recipe->fmt_dy, false, ws + p.gt, Mp, f32(p.sgt), amax_g};
+    const fp8k::GroupedColOperand cx{x, T, K, row_token, M, K, recipe->fmt_x, false, ws + p.xt, Mp, f32(p.sxt), amax_x};
+    const bool strips_w = fp8k::grouped_strips(cw, E), strips_gx = fp8k::grouped_strips(cg, E);
+    {
+        uint32_t *from = dx && !strips_w ? amax_w : amax_g, *to = dw && !strips_gx ? amax_x + E * K : amax_g;
+        if (from < to) FP8_TRY(fp8k::launch_fill_u32(from, to - from, 0u, st));
+    }
     if (dx) {
-        if (fp8k::grouped_strips(cw, E)) FP8_TRY(fp8k::launch_quant_strips_grouped(cw, nullptr, offsets, E, fl, st));
+        if (strips_w) FP8_TRY(fp8k::launch_quant_strips_grouped(cw, nullptr, offsets, E, fl, st));
         else FP8_TRY(fp8k::launch_quant_cols_grouped(cw, offsets, E, fl, st));
         FP8_TRY(fp8k::launch_quant_rows_gather(dy, M, N, nullptr, M, N, recipe->fmt_dy, fl, ws + p.gq, ld, f32(p.sg), st));
         FP8_TRY(fp8k::launch_gemm_fp8_grouped_rows({ws + p.gq, ld, recipe->fmt_dy, f32(p.sg), ws + p.wt, ld, recipe->fmt_w, f32(p.swt), offsets, E, M,
                                                     K, N, dx, K}, st));
     }
     if (dw) {
-        if (fp8k::grouped_strips(cg, E)) {
+        if (strips_gx) {
             FP8_TRY(fp8k::launch_quant_strips_grouped(cg, &cx, offsets, E, fl, st));
         } else {
             FP8_TRY(fp8k::launch_quant_cols_grouped(cg, offsets, E, fl, st));

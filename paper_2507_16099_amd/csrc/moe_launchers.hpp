@@ -32,7 +32,8 @@ hipError_t launch_quant_rows_gather(const void* x, int64_t T, int64_t ldx, const
 // Operands quantized per column within each group of rows and written transposed.
 //   rows of group e: [offsets[e], offsets[e + 1]) of the M rows; uniform: [e M / E, (e + 1) M / E) (M a multiple of E)
 //   qt: [cols, ld_t], the codes of a group start at the sum of the earlier groups' lengths, each padded to 128, and zero codes follow up
-//   to the next 16; uniform: [E, cols, ld_t].  scale [E, cols]; amax [E, cols]: scratch (of the first form)
+//   to the next 16; uniform: [E, cols, ld_t].  scale [E, cols], of groups that have rows; amax
+//   [E, cols]: zeros on entry (of the first form)
 struct GroupedColOperand {
     const void* x; int64_t T, ldx; const int32_t* row_token; int64_t M, cols; int fmt; bool uniform;
     uint8_t* qt; int64_t ld_t; float* scale; uint32_t* amax;

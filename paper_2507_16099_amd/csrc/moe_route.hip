@@ -89,11 +89,15 @@ __device__ void choose(const RouteArgs& a, int t0, int t1, int* hist) {
     const int l = threadIdx.x % LANES, sub = threadIdx.x / LANES;
     const int first_lane = (threadIdx.x & 63) - l;
     const uint64_t mine = (LANES == 64 ? ~0ull : (1ull << (LANES & 63)) - 1) << first_lane;
+    float next[VPL];
+    load_token<LANES, VPL>(a.logits, a.f32, t0 + sub < t1 ? t0 + sub : t1 - 1, a.ld, a.E, l, next);
     for (int tb = t0; tb < t1; tb += NT / LANES) {
-        const int t = tb + sub;
+        const int t = tb + sub, t_next = t + NT / LANES;
         const bool live = t < t1;
         float x[VPL];
-        load_token<LANES, VPL>(a.logits, a.f32, live ? t : t1 - 1, a.ld, a.E, l, x);
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) x[i] = next[i];
+        if (tb + NT / LANES < t1) load_token<LANES, VPL>(a.logits, a.f32, t_next < t1 ? t_next : t1 - 1, a.ld, a.E, l, next);
         uint32_t o[VPL];
 #pragma unroll
         for (int i = 0; i < VPL; ++i) o[i] = order_of(x[i]);
@@ -150,11 +154,13 @@ __device__ void place(const RouteArgs& a, int64_t s0, int64_t s1, const int* bas
     }
     __syncthreads();
     for (int e = threadIdx.x; e < E; e += NT) {
-        int at = base[e];
+        int at = base[e], n[16];
+#pragma unroll
+        for (int w = 0; w < 16; ++w) n[w] = hist[w * E + e];
+#pragma unroll
         for (int w = 0; w < 16; ++w) {
-            const int n = hist[w * E + e];
             hist[w * E + e] = at;
-            at += n;
+            at += n[w];
         }
     }
     __syncthreads();
@@ -236,6 +242,7 @@ __global__ __launch_bounds__(NT) void route_place_kernel(RouteArgs a) {
         const int lanes = a.E < NT ? a.E : NT, groups = NT / lanes, g = threadIdx.x / lanes, l = threadIdx.x % lanes;
         if (g < groups) {
             int sum = 0, sum_before = 0;
+#pragma unroll 8
             for (int c = g; c < chunks; c += groups) {
                 const int n = a.counts[(int64_t)c * a.E + l];
                 sum += n;
@@ -269,6 +276,8 @@ __global__ __launch_bounds__(256) void route_bwd_kernel(const float* __restrict_
     const int t = (int)(blockIdx.x * (256 / LANES) + threadIdx.x / LANES);
     const bool live = t < T;
     const int64_t tt = live ? t : T - 1;
+    float x[VPL];
+    if (!renorm) load_token<LANES, VPL>(logits, f32, tt, ld, E, l, x);
     // slots of the token in its first k lanes (LANES >= k)
     const int my_expert = l < k ? experts[tt * k + l] : -1;
     const float g = my_expert >= 0 ? gates[tt * k + l] : 0.f, dg = my_expert >= 0 ? dgates[tt * k + l] : 0.f;
@@ -278,8 +287,6 @@ __global__ __launch_bounds__(256) void route_bwd_kernel(const float* __restrict_
 #pragma unroll
         for (int i = 0; i < VPL; ++i) d[i] = 0.f;
     } else {
-        float x[VPL];
-        load_token<LANES, VPL>(logits, f32, tt, ld, E, l, x);
         uint32_t o = 0;
 #pragma unroll
         for (int i = 0; i < VPL; ++i) { const uint32_t oi = order_of(x[i]); o = oi > o ? oi : o; }

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from tests import moe_reference as ref
+from tests.gpu_util import knobs
 
 pytestmark = pytest.mark.gpu
 
@@ -164,6 +165,9 @@ GROUPS = [
     ([2] * 70 + [0] * 3 + [9], 100, 128, 96, 1),
     ([511, 1, 513], 1000, 1040, 528, 0),
     ([90, 1200], 600, 784, 1040, 3),
+    ([0, 5, 0, 1, 0, 2] * 52, 200, 64, 112, 7),      # more groups than are looked up at a time
+    ([3000, 1], 1500, 80, 160, 0),                   # a group that does not stay in registers
+    ([20] * 40, 300, 96, 272, 0),
 ]
 RECIPES = {"row": {}, "pow2": {"flags": 1}, "swapped": {"fmt_x": 1, "fmt_w": 1, "fmt_dy": 0}}
 
@@ -224,9 +228,36 @@ def test_few_rows_against_quantized_weights(case, recipe):
     fp8.fp8_grouped_linear_fwd_prequantized(x.cuda(), wq.view(E, N, K + 16)[:, :, :K], r.fmt_w, sw.view(E, N), offsets.cuda(), r.fmt_x, r.flags,
                                             row_token=row_token.cuda(), y=y)
     ref.assert_product(y.cpu(), want, size)
+    # every form that takes such a call: quantization inside the product, tiles of every size, persistent workgroups
+    for switches in ({"SKINNY_DMA": 2}, *({"SKINNY_DMA": 0, "GEMM_RING": 1 + f} for f in range(6)), {"SKINNY_DMA": 0, "GEMM_STREAM": 2},
+                     {"SKINNY_DMA": 0, "GEMM_STREAM": 8}):
+        with knobs(**switches):
+            other = torch.full_like(y, float("nan"))
+            fp8.fp8_grouped_linear_fwd_prequantized(x.cuda(), wq.view(E, N, K + 16)[:, :, :K], r.fmt_w, sw.view(E, N), offsets.cuda(), r.fmt_x,
+                                                    r.flags, row_token=row_token.cuda(), y=other)
+            ref.assert_product(other.cpu(), want, size)
     if not tail and case % 2:      # the rows as they are
         y2 = fp8.fp8_grouped_linear_fwd_prequantized(xr.cuda(), wq.view(E, N, K + 16)[:, :, :K], r.fmt_w, sw.view(E, N), offsets.cuda(), r.fmt_x, r.flags)
         assert torch.equal(y.view(torch.int16), y2.view(torch.int16))
+
+
+@pytest.mark.parametrize("case", range(len(GROUPS)))
+def test_every_form_of_the_products(case):
+    """Tiles of every size, and few persistent workgroups that walk many tiles: the same results within the sums' bounds."""
+    sizes, T, K, N, tail = GROUPS[case]
+    r = fp8.Recipe(gran=fp8.FP8_ROW)
+    offsets, row_token, x, w, dy = _case(sizes, T, K, N, 300 + case, tail)
+    xr = ref.rows_of(x, row_token)
+    want, size = ref.grouped_fwd(xr, w, offsets, ref.E4M3, ref.E4M3, False)
+    (want_dx, size_dx), (want_dw, size_dw) = ref.grouped_bwd(dy, xr, w, offsets, ref.E5M2, ref.E4M3, ref.E4M3, False)
+    args = (x.cuda(), w.cuda(), offsets.cuda(), r)
+    for switches in (*({"GEMM_RING": 1 + f, "GEMM_STREAM": 0} for f in range(6)), {"GEMM_STREAM": 2}, {"GEMM_STREAM": 8}):
+        with knobs(**switches):
+            y = fp8.fp8_grouped_linear_fwd(*args, row_token=row_token.cuda())
+            dx, dw = fp8.fp8_grouped_linear_bwd(dy.cuda(), *args, row_token=row_token.cuda())
+            ref.assert_product(y.cpu(), want, size)
+            ref.assert_product(dx.cpu(), want_dx, size_dx)
+            ref.assert_product(dw.cpu(), want_dw, size_dw)
 
 
 @pytest.mark.parametrize("offsets", [[0, 50, 20, 90, 200, -5], [0, -3, -4, 1 << 30, 7, 100], [7, 7, 7, 7, 7, 7], [0, 2147483647, -2147483648, 60, 40, 100]])
