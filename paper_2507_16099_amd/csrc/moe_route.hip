@@ -6,7 +6,9 @@
 //   rows: the slots (t, j) that have an expert, in the order of (expert, t, j)
 //
 // Choice: LANES lanes hold a token's logits, VPL each, as unsigned integers that order like the values (0: not to be chosen).  A
-// round takes their maximum and the lowest expert that has it: k rounds of a register reduction and a ballot.
+// round takes their maximum and the lowest expert that has it: two reductions in registers, k rounds.  Sixteen lanes a token, with
+// as many logits a lane as that takes: the vector ALU's instructions are what 16384 tokens take (one token a wavefront, 64 experts, six
+// choices 10.6 us).
 // Lists: a chunk of consecutive tokens per workgroup.  The first launch leaves each chunk's count per expert; the second adds up
 // what lies before its chunk and ranks its own slots, 64 at a time: lanes with the same expert find each other with one ballot per
 // bit of the expert's number, so ranks, and the lists, come out in order and alike every time, without atomics on positions.
@@ -60,6 +62,10 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
     return lanes_fold<LANES>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }
 template <int LANES>
+__device__ __forceinline__ uint32_t lanes_min(uint32_t v) {
+    return lanes_fold<LANES>(v, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+}
+template <int LANES>
 __device__ __forceinline__ float lanes_sum(float v) {
     return __uint_as_float(lanes_fold<LANES>(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
 }
@@ -87,8 +93,7 @@ struct RouteArgs {
 template <int LANES, int VPL>
 __device__ void choose(const RouteArgs& a, int t0, int t1, int* hist) {
     const int l = threadIdx.x % LANES, sub = threadIdx.x / LANES;
-    const int first_lane = (threadIdx.x & 63) - l;
-    const uint64_t mine = (LANES == 64 ? ~0ull : (1ull << (LANES & 63)) - 1) << first_lane;
+    constexpr uint32_t NONE = 0xFFFFu;
     float next[VPL];
     load_token<LANES, VPL>(a.logits, a.f32, t0 + sub < t1 ? t0 + sub : t1 - 1, a.ld, a.E, l, next);
     for (int tb = t0; tb < t1; tb += NT / LANES) {
@@ -108,15 +113,13 @@ __device__ void choose(const RouteArgs& a, int t0, int t1, int* hist) {
 #pragma unroll
             for (int i = 1; i < VPL; ++i) best = o[i] > best ? o[i] : best;
             best = lanes_max<LANES>(best);
-            int expert = -1;
+            uint32_t lowest = NONE;      // of this lane's experts that have it
 #pragma unroll
-            for (int i = VPL - 1; i >= 0; --i) {
-                const uint64_t has = __ballot(best != 0 && o[i] == best) & mine;
-                if (has) expert = LANES * i + __ffsll((unsigned long long)has) - 1 - first_lane;
-            }
+            for (int i = VPL - 1; i >= 0; --i) lowest = o[i] == best ? (uint32_t)(l + LANES * i) : lowest;
+            lowest = lanes_min<LANES>(lowest);
+            const int expert = best ? (int)lowest : -1;
 #pragma unroll
-            for (int i = 0; i < VPL; ++i)
-                if (expert == l + LANES * i) o[i] = 0u;
+            for (int i = 0; i < VPL; ++i) o[i] = lowest == (uint32_t)(l + LANES * i) ? 0u : o[i];
             if (j == 0) {
                 top = best ? value_of(best) : 0.f;
                 float s = 0.f;
@@ -333,10 +336,10 @@ size_t route_workspace_bytes(int64_t T, int64_t E) { return one_chunk(T) ? 256 :
 
 #define FP8K_ROUTE_FORMS(E_, CALL)          \
     if (E_ <= 16) { CALL(16, 1); }          \
-    else if (E_ <= 32) { CALL(32, 1); }     \
-    else if (E_ <= 64) { CALL(64, 1); }     \
-    else if (E_ <= 128) { CALL(64, 2); }    \
-    else if (E_ <= 256) { CALL(64, 4); }    \
+    else if (E_ <= 32) { CALL(16, 2); }     \
+    else if (E_ <= 64) { CALL(16, 4); }     \
+    else if (E_ <= 128) { CALL(16, 8); }    \
+    else if (E_ <= 256) { CALL(32, 8); }    \
     else { CALL(64, 8); }
 
 hipError_t launch_moe_route(const void* logits, bool f32, int64_t T, int64_t E, int64_t ld, int k, bool renorm, float* gates, int32_t* experts,
