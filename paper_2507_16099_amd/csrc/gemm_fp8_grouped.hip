@@ -1,15 +1,19 @@
 // Scaled FP8 products grouped by expert (gfx950), groups of any size that only the device knows:
 //   rows      out[r] = A[r] B[e]^T / (sa[r] sb[e])        for the rows r of group e; one weight B[e] [N, K] per group
 //   contract  out[e] = A_e B_e^T / (sa[e] sb[e])          A_e [N, n_e], B_e [K, n_e]: the columns of the group in A [N, lda], B [K, ldb]
-// The tile kernel is that of gemm_fp8_ring.hpp: a ring of R stages of K steps filled by LDS-DMA ahead of the matrix cores, one
-// workgroup barrier a step, fragments of the next step read behind the matrix instructions of the present one; its LDS layout,
-// swizzle keys and operand order are described there.
+// The K step is that of gemm_fp8_ring.hpp: a ring of R stages filled by LDS-DMA ahead of the matrix cores, one workgroup barrier a step,
+// fragments of the next step read behind the matrix instructions of the present one; LDS layout, swizzle keys and operand
+// order are described there.
 //
-// What is different: which tile a workgroup has.  The host knows M rows and E groups, so it launches as many workgroups as the
-// groups can come to (rows: M / TM + E row tiles); each finds its tile by a scan of the offsets over the lanes of a wavefront, and
-// those beyond the last tile end.  The tiles in use are dealt to the XCDs in contiguous ranges, walked in patches of GROUP_M row
-// tiles, as in the ungrouped kernels; neighbouring row tiles of one group share the weight's panel in that L2.
-// Rows behind the last group (slots that no expert took) are written as zeros: a tile without K steps.
+// What is different: a workgroup walks many tiles and its ring never drains.  The refills run R steps ahead of the matrix instructions
+// through the sequence of all steps of all its tiles, so that a tile's first operands arrive while the tile before it is computed; an
+// expert's product is 4 to 32 steps long, and filling the ring for each tile again cost 3 to 5 us, as much as eight steps.
+// Scales and the tile's place come a tile ahead in the same way, into one of R + 2 tables.  The epilogue goes from registers to memory:
+// the lanes of a row exchange halves until each store instruction writes 64 bytes of it.
+//
+// Which tiles: the host knows M rows and E groups; the workgroup reads the offsets and leaves in LDS where each group's rows start and how
+// many tiles lie before it.  Tiles go round the workgroups in patches of GROUP_M row tiles, eight XCDs side by side (see
+// gemm_fp8_grouped_stream.hip).  Rows behind the last group (slots that no expert took) are written as zeros: a tile without codes.
 #include "gemm_fp8_ring.hpp"
 #include "group_tiles.hpp"
 #include "moe_launchers.hpp"
@@ -29,6 +33,7 @@ struct GroupedArgs {
     uint16_t* out; int64_t ld_out;
     int tiles_n, tiles_m;        // tiles_m: of one group's output (contract)
 };
+typedef unsigned v2u_gr __attribute__((ext_vector_type(2)));
 
 template <int FA, int FB, int TM, int TN, int WAVES_M, int WAVES_N, int R, int GROUP_M, bool CONTRACT>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void gemm_fp8_grouped_kernel(GroupedArgs p) {
@@ -43,95 +48,95 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void gemm_fp8_grouped_kerne
     constexpr int UA = (TM + 63) / 64, TMS = 64 * UA, NU = UA + TN / 64;
     constexpr int NLA = TM / (8 * NW), NLB = TN / (8 * NW), NL = NLA + NLB;
     constexpr int NM = FM * FN;
-    constexpr bool ACC_V = 4 * NM + 16 * (FM + FN) <= (NW == 8 ? 208 : 192);
-    static_assert((NW == 4 || NW == 8) && WM % 16 == 0 && (GW == 64 || GW == 32) && WN % GW == 0 && TM % (8 * NW) == 0 && TN % 64 == 0 && TN % (8 * NW) == 0, "tile");
-    static_assert(R >= 3 && (R - 1) * NL <= 63, "vmcnt range");
-    constexpr int CPR = WN / 8;
-    constexpr bool POW2 = (CPR & (CPR - 1)) == 0;
-    constexpr int PITCH = (CPR + (POW2 ? 0 : 1)) * 16;
-    static_assert(NW * WM * PITCH <= R * STAGE, "the epilogue stages through the ring");
+    constexpr bool ACC_V = 4 * NM + 16 * (FM + FN) <= 176;
+    constexpr int NTAB = R + 2, TAB = NU * 64;       // tables of scales: a tile's and those of the R + 1 tiles that may be entered before it is done
+    static_assert(NW == 4 && WM % 16 == 0 && (GW == 64 || GW == 32) && WN % GW == 0 && TM % (8 * NW) == 0 && TN % 64 == 0, "tile");
+    static_assert(R >= 3 && (R - 1) * NL <= 63 && TM <= 256 && TN <= 256, "vmcnt range, a scale per thread");
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-
-    const int slot = (int)blockIdx.x / NUM_XCD, xcd = (int)blockIdx.x % NUM_XCD;
-    int group, m0, n0, rows_a, rows_b, Kt;         // Kt: contracted elements (codes)
-    const uint8_t *a0, *b0;
-    const float *sa, *sb;
-    uint16_t* out;
-    if constexpr (!CONTRACT) {
-        GroupTile t = find_group_tile<true>(p.offsets, p.E, p.M, TM, -1);
-        const int tiles = t.total * p.tiles_n, per_xcd = (tiles + NUM_XCD - 1) / NUM_XCD;
-        const int logical = xcd * per_xcd + slot;
-        if (slot >= per_xcd || logical >= tiles) return;
-        const int in_group = GROUP_M * p.tiles_n, first_m = logical / in_group * GROUP_M, in = logical % in_group;
-        const int gsize = t.total - first_m < GROUP_M ? t.total - first_m : GROUP_M;
-        const int tn = in / gsize, tm = first_m + in - tn * gsize;
-        t = find_group_tile<true>(p.offsets, p.E, p.M, TM, tm);
-        group = t.group;
-        const int e = group < p.E ? group : p.E - 1;
-        m0 = t.row0;
-        rows_a = t.rows;
-        n0 = tn * TN;
-        rows_b = p.N - n0 < TN ? p.N - n0 : TN;
-        Kt = group < p.E ? p.K : 0;
-        a0 = p.A + (int64_t)m0 * p.lda;
-        b0 = p.B + ((int64_t)e * p.N + n0) * p.ldb;
-        sa = p.scale_a + m0;
-        sb = p.scale_b + (int64_t)e * p.N + n0;
-        out = p.out + (int64_t)m0 * p.ld_out;
-    } else {
-        const int per_group = p.tiles_m * p.tiles_n;
-        const int64_t tiles = (int64_t)per_group * p.E, per_xcd = (tiles + NUM_XCD - 1) / NUM_XCD;
-        const int64_t logical = xcd * per_xcd + slot;
-        if (slot >= per_xcd || logical >= tiles) return;
-        group = (int)(logical / per_group);
-        const int rest = (int)(logical % per_group);
-        const int in_group = GROUP_M * p.tiles_n, first_m = rest / in_group * GROUP_M, in = rest % in_group;
-        const int gsize = p.tiles_m - first_m < GROUP_M ? p.tiles_m - first_m : GROUP_M;
-        const int tn = in / gsize, tm = first_m + in - tn * gsize;
-        const GroupSpan s = find_group(p.offsets, p.E, p.M, group);
-        m0 = tm * TM;
-        n0 = tn * TN;
-        rows_a = p.N - m0 < TM ? p.N - m0 : TM;
-        rows_b = p.K - n0 < TN ? p.K - n0 : TN;
-        Kt = (s.rows + 15) & ~15;
-        a0 = p.A + (int64_t)m0 * p.lda + s.pad0;
-        b0 = p.B + (int64_t)n0 * p.ldb + s.pad0;
-        sa = p.scale_a + (int64_t)group * p.N + m0;
-        sb = p.scale_b + (int64_t)group * p.K + n0;
-        out = p.out + ((int64_t)group * p.N + m0) * p.ld_out;
-    }
-    const int cols = CONTRACT ? p.K : p.N;
+    float* const tabs = reinterpret_cast<float*>(smem + R * STAGE);
+    int4* const places = reinterpret_cast<int4*>(tabs + NTAB * TAB);      // of those tiles: first row, rows, first column, contracted codes
+    int* const starts = reinterpret_cast<int*>(places + NTAB);            // [E + 2] each
+    int *const tiles_to = starts + p.E + 2, *const pads = tiles_to + p.E + 2;
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm0 = (wave / WAVES_N) * WM, wn0 = (wave % WAVES_N) * WN;
+    if (wave == 0) list_groups(p.offsets, p.E, p.M, TM, starts, tiles_to, pads);
+    __syncthreads();
 
+    // ---- this workgroup's tiles
+    const int tiles_n = p.tiles_n, per_group = p.tiles_m * tiles_n;
+    const int row_tiles = CONTRACT ? p.tiles_m * p.E : __builtin_amdgcn_readfirstlane(tiles_to[p.E + 1]);
+    const int units = row_tiles * tiles_n;
+    const int slots = (int)gridDim.x / NUM_XCD;
+    const int u_first = ((int)blockIdx.x % NUM_XCD) * slots + (int)blockIdx.x / NUM_XCD, u_step = NUM_XCD * slots;
+    if (u_first >= units) return;
+    const int cols_all = CONTRACT ? p.K : p.N;
     const int64_t lda = p.lda, ldb = p.ldb;
-    const uint64_t pa = reinterpret_cast<uint64_t>(a0), pb = reinterpret_cast<uint64_t>(b0);
-    const v4i_t rsrc_a = {(int)(uint32_t)pa, (int)(uint32_t)(pa >> 32), (int)((int64_t)(rows_a - 1) * lda + Kt), 0x00020000};
-    const v4i_t rsrc_b = {(int)(uint32_t)pb, (int)(uint32_t)(pb >> 32), (int)((int64_t)(rows_b - 1) * ldb + Kt), 0x00020000};
 
-    float* inv_tab = reinterpret_cast<float*>(smem + R * STAGE);
-    {
-        const uint64_t psa = reinterpret_cast<uint64_t>(sa), psb = reinterpret_cast<uint64_t>(sb);
-        const v4i_t rsrc_sa = {(int)(uint32_t)psa, (int)(uint32_t)(psa >> 32), rows_a * 4, 0x00020000};
-        const v4i_t rsrc_sb = {(int)(uint32_t)psb, (int)(uint32_t)(psb >> 32), rows_b * 4, 0x00020000};
-#pragma unroll
-        for (int h = 0; h < (NU + NW - 1) / NW; ++h) {
-            const int u = wave + NW * h, r = 64 * (u < UA ? u : u - UA) + lane;
-            const uint32_t at = (uint32_t)(size_t)inv_tab + (uint32_t)u * 256u;
-            if (u < UA) lds_dma4(rsrc_sa, at, (uint32_t)(r < rows_a ? r : rows_a - 1) * 4u);
-            else if (u < NU) lds_dma4(rsrc_sb, at, (uint32_t)(r < rows_b ? r : rows_b - 1) * 4u);
+    // ---- the tile whose operands are requested next: its panels, contracted codes, the step's first code
+    v4i_t rsrc_a, rsrc_b;
+    int k_tile = 0, k_next = 0, u_next = u_first, tab_next = 0;
+    auto enter_tile = [&] {
+        int row = 0, rows = 1, n0 = 0, brow = 0;
+        uint64_t pa = reinterpret_cast<uint64_t>(p.A), pb = reinterpret_cast<uint64_t>(p.B);
+        const bool real = u_next < units;
+        k_tile = 0;
+        k_next = 0;
+        if (real) {
+            const int e_c = CONTRACT ? u_next / per_group : 0;
+            const int rest = u_next - e_c * per_group, in_group = GROUP_M * tiles_n, most_m = CONTRACT ? p.tiles_m : row_tiles;
+            const int first_m = rest / in_group * GROUP_M, in = rest % in_group;
+            const int gsize = most_m - first_m < GROUP_M ? most_m - first_m : GROUP_M;
+            const int tm = first_m + in % gsize;
+            n0 = in / gsize * TN;
+            if constexpr (CONTRACT) {
+                const int start = __builtin_amdgcn_readfirstlane(starts[e_c]), pad0 = __builtin_amdgcn_readfirstlane(pads[e_c]);
+                k_tile = (__builtin_amdgcn_readfirstlane(starts[e_c + 1]) - start + 15) & ~15;
+                const int m0 = tm * TM;
+                row = e_c * p.N + m0;
+                rows = p.N - m0 < TM ? p.N - m0 : TM;
+                brow = e_c * p.K + n0;
+                pa = reinterpret_cast<uint64_t>(p.A + (int64_t)m0 * lda + pad0);
+                pb = reinterpret_cast<uint64_t>(p.B + (int64_t)n0 * ldb + pad0);
+            } else {
+                const int e = group_of_tile(tiles_to, p.E, tm);
+                row = __builtin_amdgcn_readfirstlane(starts[e]) + (tm - __builtin_amdgcn_readfirstlane(tiles_to[e])) * TM;
+                rows = __builtin_amdgcn_readfirstlane(starts[e + 1]) - row;
+                if (rows > TM) rows = TM;
+                k_tile = e < p.E ? p.K : 0;
+                brow = (e < p.E ? e : p.E - 1) * p.N + n0;
+                pa = reinterpret_cast<uint64_t>(p.A + (int64_t)row * lda);
+                pb = reinterpret_cast<uint64_t>(p.B + (int64_t)brow * ldb);
+            }
         }
-    }
-    auto scale_table = [&]() {       // (a tile without K steps is zero whatever stands in its scales)
-        if (tid < TM) inv_tab[tid] = Kt ? 1.0f / inv_tab[tid] : 0.0f;
-        if (tid < TN) inv_tab[TMS + tid] = Kt ? 1.0f / inv_tab[TMS + tid] : 0.0f;
+        const int cols = cols_all - n0 < TN ? cols_all - n0 : TN;
+        rsrc_a = v4i_t{(int)(uint32_t)pa, (int)(uint32_t)(pa >> 32), (int)((int64_t)(rows - 1) * lda + k_tile), 0x00020000};
+        rsrc_b = v4i_t{(int)(uint32_t)pb, (int)(uint32_t)(pb >> 32), (int)((int64_t)(cols - 1) * ldb + k_tile), 0x00020000};
+        if (real) {
+            const uint64_t psa = reinterpret_cast<uint64_t>(p.scale_a + row), psb = reinterpret_cast<uint64_t>(p.scale_b + brow);
+            const v4i_t rsrc_sa = {(int)(uint32_t)psa, (int)(uint32_t)(psa >> 32), rows * 4, 0x00020000};
+            const v4i_t rsrc_sb = {(int)(uint32_t)psb, (int)(uint32_t)(psb >> 32), cols * 4, 0x00020000};
+#pragma unroll
+            for (int h = 0; h < (NU + NW - 1) / NW; ++h) {
+                const int u = wave + NW * h, r = 64 * (u < UA ? u : u - UA) + lane;
+                const uint32_t at = (uint32_t)(size_t)(tabs + tab_next * TAB) + (uint32_t)u * 256u;
+                if (u < UA) lds_dma4(rsrc_sa, at, (uint32_t)(r < rows ? r : rows - 1) * 4u);
+                else if (u < NU) lds_dma4(rsrc_sb, at, (uint32_t)(r < cols ? r : cols - 1) * 4u);
+            }
+        }
+        if (tid == 0) places[tab_next] = make_int4(row, rows, n0, k_tile);
+        u_next += u_step;
+        tab_next = tab_next + 1 == NTAB ? 0 : tab_next + 1;
+    };
+    auto advance = [&] {      // to the next step of the sequence (a tile without codes has one, of zeros)
+        k_next += BK;
+        if (k_next >= k_tile) enter_tile();
     };
 
     const int lrow = lane >> 3;
     const int ca = (lane & 7) ^ ((4 * (wave & 1) + (lrow >> 1)) & 7);
-    const int kb_e = SH == 4 ? (wave >> 1) : wave, kb_o = SH == 4 && NW == 4 ? 2 + (wave >> 1) : kb_e;
+    const int kb_e = SH == 4 ? (wave >> 1) : wave, kb_o = SH == 4 ? 2 + (wave >> 1) : kb_e;
     const int cb_e = (lane & 7) ^ (((lrow >> 1) & 1) | ((kb_e & 3) << 1));
     const int cb_o = (lane & 7) ^ (((lrow >> 1) & 1) | ((kb_o & 3) << 1));
     const uint32_t va0 = (uint32_t)((wave * 8 + lrow) * (int)lda + ca * 16);
@@ -144,7 +149,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void gemm_fp8_grouped_kerne
         if (q < NLB) lds_dma16<>(rsrc_b, lds_base + stage_off + TM * BK + q * (NW * 1024), ((q & 1) ? vb0_o + ko : vb0_e + ke) + (uint32_t)q * vb_step);
         else if (q < NL) lds_dma16<>(rsrc_a, lds_base + stage_off + (q - NLB) * (NW * 1024), va0 + (uint32_t)(q - NLB) * va_step + ka);
     };
-    auto kofs = [&](int k0, int c) { return k0 + c * 16 < Kt ? (uint32_t)k0 : OOB; };
+    auto kofs = [&](int c) { return k_next + c * 16 < k_tile ? (uint32_t)k_next : OOB; };
 
     const int r16 = lane & 15, g = lane >> 4;
     const int key_a = (r16 >> 1) & 7;
@@ -167,40 +172,41 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void gemm_fp8_grouped_kerne
     };
 
     v4f_t acc[FM][FN];
+    auto clear = [&] {      // (the vector ALU's writes, two wait states ahead of any matrix instruction)
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = v4f_t{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < NM; ++i) {
+            acc[i / FN][i % FN] = v4f_t{0.f, 0.f, 0.f, 0.f};
+            if constexpr (ACC_V) asm volatile("" : "+v"(acc[i / FN][i % FN]));
+            else asm volatile("" : "+a"(acc[i / FN][i % FN]));
+        }
+        asm volatile("s_nop 3" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
 
-    const int ksteps = (Kt + BK - 1) / BK;
     using I0 = std::integral_constant<int, 0>;
     using I1 = std::integral_constant<int, 1>;
-#pragma unroll
+    enter_tile();
+#pragma unroll 1
     for (int r = 0; r < R; ++r) {
-        const int k0 = r * BK;
-        const uint32_t ka = kofs(k0, ca), ke = kofs(k0, cb_e), ko = kofs(k0, cb_o);
+        const uint32_t ka = kofs(ca), ke = kofs(cb_e), ko = kofs(cb_o);
 #pragma unroll
         for (int q = 0; q < NL; ++q) load_q(q, (uint32_t)(r * STAGE), ka, ke, ko);
+        advance();
     }
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int i = 0; i < NM; ++i) {
-        if constexpr (ACC_V) asm volatile("" : "+v"(acc[i / FN][i % FN]));
-        else asm volatile("" : "+a"(acc[i / FN][i % FN]));
-    }
-    wait_vmem_but_barrier<(R - 1) * NL>();
+    clear();
+    wait_vmem_but_barrier<(R - 1) * NL>();      // stage 0 has landed for everyone (scale loads in between: the wait is the stricter)
 #pragma unroll
     for (int q = 0; q < FM + FN; ++q) read_q(I0{}, smem, q);
-    scale_table();
     __builtin_amdgcn_sched_barrier(0);
 
     uint32_t cur = 0, nxt = STAGE;
-    int k_refill = R * BK;
     auto step = [&](auto par_t) {
         constexpr int P = decltype(par_t)::value;
         using NS = std::integral_constant<int, P ^ 1>;
+        // (operations younger than stage s + 1's loads: those of R - 2 stages, and now and then scale loads and stores, with which the
+        // wait is stricter than it need be)
         wait_vmem_but_barrier<(R - 2) * NL>();
-        const uint32_t ka = kofs(k_refill, ca), ke = kofs(k_refill, cb_e), ko = kofs(k_refill, cb_o);
+        const uint32_t ka = kofs(ca), ke = kofs(cb_e), ko = kofs(cb_o), to = (uint32_t)__builtin_amdgcn_readfirstlane((int)cur);
         const uint8_t* rs = smem + nxt;
         constexpr int QR = NM >= 16 ? NM * 5 / 8 : (NM + 1) / 2;
 #pragma unroll
@@ -212,91 +218,106 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void gemm_fp8_grouped_kerne
                 for (int q = t * (FM + FN) / QR; q < (t + 1) * (FM + FN) / QR; ++q) read_q(NS{}, rs, q);
             }
 #pragma unroll
-            for (int q = t * NL / NM; q < (t + 1) * NL / NM; ++q) load_q(q, cur, ka, ke, ko);
+            for (int q = t * NL / NM; q < (t + 1) * NL / NM; ++q) load_q(q, to, ka, ke, ko);
             __builtin_amdgcn_sched_barrier(0);
         }
         cur = nxt;
         nxt = nxt + STAGE == R * STAGE ? 0 : nxt + STAGE;
-        k_refill += BK;
+        advance();
     };
-    int s = 0;
-    if constexpr (ACC_V) {
-        for (; s + 2 <= ksteps; s += 2) {
-            step(I0{});
-            step(I1{});
-        }
-        if (s < ksteps) step(I0{});
-    } else {
-        do {
-            step(I0{});
-            if (s + 1 < ksteps) step(I1{});
-            s += 2;
-        } while (s < ksteps);
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
 
-    constexpr int CE = GW / 4;
-    float inv_b[NG][CE];
-#pragma unroll
-    for (int grp = 0; grp < NG; ++grp)
-#pragma unroll
-        for (int e = 0; e < CE; e += 4) {
-            const float4 t4 = *reinterpret_cast<const float4*>(inv_tab + TMS + wn0 + GW * grp + CE * g + e);
-            inv_b[grp][e] = t4.x; inv_b[grp][e + 1] = t4.y; inv_b[grp][e + 2] = t4.z; inv_b[grp][e + 3] = t4.w;
-        }
-    float inv_a[FM];
-#pragma unroll
-    for (int fi = 0; fi < FM; ++fi) inv_a[fi] = inv_tab[wm0 + 16 * fi + r16];
-    uint8_t* q_lds = smem + wave * (WM * PITCH);
-#pragma unroll
-    for (int fi = 0; fi < FM; ++fi) {
-        uint8_t* row = q_lds + (16 * fi + r16) * PITCH;
+    // ---- a tile's end: reciprocals of its scales, the results, and on to the next one
+    int tab = 0, u = u_first, left = 0;      // left: steps of the present tile to go
+    auto steps_of = [&](int slot) {
+        const int k = __builtin_amdgcn_readfirstlane(places[slot].w);
+        return k > BK ? (k + BK - 1) / BK : 1;
+    };
+    const uint32_t lane_out = (uint32_t)(((wm0 + r16) * (int)p.ld_out + wn0 + 8 * g) * 2);
+    auto finish = [&] {
+        float* const t = tabs + tab * TAB;
+        const int4 at = places[tab];
+        const int row = __builtin_amdgcn_readfirstlane(at.x), rows = __builtin_amdgcn_readfirstlane(at.y), n0 = __builtin_amdgcn_readfirstlane(at.z);
+        const bool some = __builtin_amdgcn_readfirstlane(at.w) != 0;      // (a tile without codes is zero whatever stands in its scales)
+        if (tid < TM) t[tid] = some ? 1.0f / t[tid] : 0.0f;
+        if (tid < TN) t[TMS + tid] = some ? 1.0f / t[TMS + tid] : 0.0f;
+        asm volatile("s_nop 15\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        const int cols = cols_all - n0 < TN ? cols_all - n0 : TN;
+        const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(p.out + (int64_t)row * p.ld_out + n0, 0,
+                                                                             (int)(((int64_t)(rows - 1) * p.ld_out + cols) * 2), 0x00020000);
+        constexpr int CE = GW / 4;      // consecutive columns of a lane in a group
 #pragma unroll
         for (int grp = 0; grp < NG; ++grp) {
-            float v[CE];
+            float inv_b[CE];
 #pragma unroll
-            for (int e = 0; e < CE; ++e) v[e] = (acc[fi][grp * GT + (e >> 2)][e & 3] * inv_a[fi]) * inv_b[grp][e];
+            for (int e = 0; e < CE; e += 4) {
+                const float4 t4 = *reinterpret_cast<const float4*>(t + TMS + wn0 + GW * grp + CE * g + e);
+                inv_b[e] = t4.x; inv_b[e + 1] = t4.y; inv_b[e + 2] = t4.z; inv_b[e + 3] = t4.w;
+            }
 #pragma unroll
-            for (int h = 0; h < CE / 8; ++h) {
-                const int c = (GW / 8) * grp + (CE / 8) * g + h;
-                *reinterpret_cast<uint4*>(row + ((POW2 ? c ^ (r16 % CPR) : c) << 4)) =
-                    make_uint4(pack_bf16(v[8 * h], v[8 * h + 1]), pack_bf16(v[8 * h + 2], v[8 * h + 3]),
-                               pack_bf16(v[8 * h + 4], v[8 * h + 5]), pack_bf16(v[8 * h + 6], v[8 * h + 7]));
+            for (int fi = 0; fi < FM; ++fi) {
+                const float inv_a = t[wm0 + 16 * fi + r16];
+                uint32_t pk[CE / 2];
+#pragma unroll
+                for (int e = 0; e < CE; e += 2)
+                    pk[e / 2] = pack_bf16((acc[fi][grp * GT + (e >> 2)][e & 3] * inv_a) * inv_b[e],
+                                          (acc[fi][grp * GT + ((e + 1) >> 2)][(e + 1) & 3] * inv_a) * inv_b[e + 1]);
+                const uint32_t off = lane_out + (uint32_t)((16 * fi * (int)p.ld_out + GW * grp) * 2);
+                const int col = wn0 + GW * grp + 8 * g;
+                if constexpr (GW == 64) {
+                    // lanes g = 0 .. 3 of a row hold its pieces (2 g, 2 g + 1) of eight columns; after the swaps pieces g and 4 + g
+                    uint32_t lo[4], hi[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const v2u_gr s1 = __builtin_amdgcn_permlane16_swap(pk[e], pk[4 + e], false, false);
+                        const v2u_gr s2 = __builtin_amdgcn_permlane32_swap(s1[0], s1[1], false, false);
+                        lo[e] = s2[0]; hi[e] = s2[1];
+                    }
+                    __builtin_amdgcn_raw_buffer_store_b128(v4u_t{lo[0], lo[1], lo[2], lo[3]}, rsrc, (int)(col < cols ? off : OOB), 0, 2);
+                    __builtin_amdgcn_raw_buffer_store_b128(v4u_t{hi[0], hi[1], hi[2], hi[3]}, rsrc, (int)(col + 32 < cols ? off + 64u : OOB), 0, 2);
+                } else {
+                    __builtin_amdgcn_raw_buffer_store_b128(v4u_t{pk[0], pk[1], pk[2], pk[3]}, rsrc, (int)(col < cols ? off : OOB), 0, 2);
+                }
             }
         }
-    }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-#pragma unroll
-    for (int fi = 0; fi < FM; ++fi) {
-#pragma unroll
-        for (int it = 0; it < (CPR + 3) / 4; ++it) {
-            const int piece = 64 * it + lane;
-            if (piece >= 16 * CPR) continue;
-            const int rr = 16 * fi + piece / CPR, c_rd = piece % CPR;
-            const uint4 v = *reinterpret_cast<const uint4*>(q_lds + rr * PITCH + ((POW2 ? c_rd ^ ((rr & 15) % CPR) : c_rd) << 4));
-            const int m = wm0 + rr, n = n0 + wn0 + c_rd * 8;
-            // (the output's columns are a multiple of eight)
-            if (m < rows_a && n < cols) *reinterpret_cast<v4u_t*>(out + (int64_t)m * p.ld_out + n) = v4u_t{v.x, v.y, v.z, v.w};
+        clear();
+        u += u_step;
+        tab = tab + 1 == NTAB ? 0 : tab + 1;
+        left = steps_of(tab);
+    };
+    left = steps_of(0);
+    while (true) {
+        step(I0{});
+        if (--left == 0) {
+            finish();
+            if (u >= units) break;
+        }
+        step(I1{});
+        if (--left == 0) {
+            finish();
+            if (u >= units) break;
         }
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // trailing (out-of-range) refills must land before the LDS is handed back
 }
 
 template <int FA, int FB, int TM, int TN, int WAVES_M, int WAVES_N, int R, int GROUP_M, bool CONTRACT>
 hipError_t launch_t(const GroupedGemm& g, hipStream_t st) {
     using namespace rg;
     auto kern = gemm_fp8_grouped_kernel<FA, FB, TM, TN, WAVES_M, WAVES_N, R, GROUP_M, CONTRACT>;
-    constexpr int lds = R * (TM + TN) * BK + ((TM + 63) / 64 + TN / 64) * 256;
-    static_assert(lds <= 160 * 1024, "LDS");
+    constexpr int lds_fixed = R * (TM + TN) * BK + (R + 2) * (((TM + 63) / 64 + TN / 64) * 256 + 16);
+    static_assert(lds_fixed + 12 * (GROUPED_MAX_EXPERTS + 2) <= 160 * 1024, "LDS");
+    const int lds = lds_fixed + 12 * (int)(g.E + 2);
     static DynamicLdsOnce attr;
-    if (hipError_t err = attr.ensure(reinterpret_cast<const void*>(kern), lds); err != hipSuccess) return err;
+    if (hipError_t err = attr.ensure(reinterpret_cast<const void*>(kern), lds_fixed + 12 * (GROUPED_MAX_EXPERTS + 2)); err != hipSuccess) return err;
     const int64_t tiles_n = ((CONTRACT ? g.K : g.N) + TN - 1) / TN, tiles_m = (g.N + TM - 1) / TM;
     // rows: each group that has rows, and what lies behind the last one, has at most one tile that is not full
-    const int64_t most = CONTRACT ? tiles_m * g.E : g.M / TM + (g.E + 1 < g.M ? g.E + 1 : g.M);
-    const int64_t tiles = most * tiles_n, grid = (tiles + NUM_XCD - 1) / NUM_XCD * NUM_XCD;
-    if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
+    const int64_t most = (CONTRACT ? tiles_m * g.E : g.M / TM + (g.E + 1 < g.M ? g.E + 1 : g.M)) * tiles_n;
+    if (most > 0x3FFFFFFF) return hipErrorInvalidValue;
+    int64_t cus = compute_units();
+    if (const int forced = knob(KNOB_GEMM_STREAM); forced >= NUM_XCD) cus = forced;      // (few workgroups walk many tiles each)
+    int64_t grid = std::max<int64_t>(cus, NUM_XCD) / NUM_XCD * NUM_XCD * (lds_fixed <= 72 * 1024 ? 2 : 1);
+    if (const int64_t need = (most + NUM_XCD - 1) / NUM_XCD * NUM_XCD; grid > need) grid = need;
     const GroupedArgs a{g.a, g.lda, g.b, g.ldb, g.scale_a, g.scale_b, g.offsets, (int)g.E, (int)g.M, (int)g.N, (int)g.K,
                         static_cast<uint16_t*>(g.out), g.ld_out, (int)tiles_n, (int)tiles_m};
     kern<<<dim3((unsigned)grid), dim3(64 * WAVES_M * WAVES_N), lds, st>>>(a);
@@ -346,7 +367,7 @@ hipError_t launch_rows(const GroupedGemm& g, hipStream_t st) {
         form = forced - 1 < F_STREAM ? forced - 1 : F_128x128;
     } else {
         const int64_t cus = compute_units() > 0 ? compute_units() : 256;
-        const bool fits = stream != 0 && gemm_fp8_grouped_stream_fits(g);
+        const bool fits = stream != 0;
         for (int f = 1; f < (fits ? FORMS : F_STREAM); ++f)
             if (form_cost(kForms[f], g, cus) < form_cost(kForms[form], g, cus)) form = f;
         if (fits && stream >= 2) form = F_STREAM;
@@ -368,12 +389,10 @@ hipError_t launch_gemm_fp8_grouped_rows(const GroupedGemm& g, hipStream_t st) {
     FP8K_FORMATS(launch_rows)
 }
 
-// dW: the persistent kernel (64 experts 1408 x 2048 of 16 .. 2048 rows: 86 to 430 us, 128 x 256 tiles 150 to 620), tiles for the
-// tables of groups that its LDS has no room for
 template <int FA, int FB>
 static hipError_t launch_contract(const GroupedGemm& g, hipStream_t st) {
-    if (knob(KNOB_GEMM_STREAM) != 0 && gemm_fp8_grouped_stream_fits(g)) return launch_gemm_fp8_grouped_stream_contract(g, st);
-    return launch_t<FA, FB, 128, 128, 2, 2, 4, 4, true>(g, st);
+    if (knob(KNOB_GEMM_STREAM) != 0) return launch_gemm_fp8_grouped_stream_contract(g, st);
+    return launch_t<FA, FB, 128, 256, 2, 2, 3, 8, true>(g, st);
 }
 hipError_t launch_gemm_fp8_grouped_contract(const GroupedGemm& g, hipStream_t st) { FP8K_FORMATS(launch_contract) }
 

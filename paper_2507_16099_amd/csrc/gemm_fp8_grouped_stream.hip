@@ -22,7 +22,7 @@ namespace fp8k {
 namespace {
 
 enum { ST_ONLY = 4 };      // a pair that is a tile's first and last
-constexpr int TABLE_GROUPS = (160 * 1024 - st::LDS_BYTES) / 12 - 2;      // what the LDS has left holds three numbers per group
+static_assert(st::LDS_BYTES + 12 * (GROUPED_MAX_EXPERTS + 2) <= 160 * 1024, "the groups' table");
 
 struct GroupedStreamArgs {
     const uint8_t* A; int64_t lda; const uint8_t* B; int64_t ldb;
@@ -62,30 +62,7 @@ __global__ __launch_bounds__(st::NT) void gemm_fp8_grouped_stream_kernel(Grouped
     // ---- the groups: starts[e] the first row, tiles_to[e] tiles of the groups before e, pads[e] the group's place in the padded order
     int* const starts = reinterpret_cast<int*>(smem + 2 * STAGE + 2 * TAB);
     int *const tiles_to = starts + p.E + 2, *const pads = tiles_to + p.E + 2;
-    if (wave == 0) {
-        int end = 0, tiles_before = 0, pad_before = 0;
-        for (int e0 = 0; e0 <= p.E; e0 += 64) {
-            const int e = e0 + lane;
-            int g_end = e < p.E ? p.offsets[e + 1] : e == p.E ? p.M : 0;
-            g_end = g_end < end ? end : g_end > p.M ? p.M : g_end;
-            g_end = wave_scan_max(g_end);
-            const int g_start = wave_before(g_end, end);
-            const int tiles = (g_end - g_start + TM - 1) / TM, pad = (g_end - g_start + 127) & ~127;
-            const int tiles_sum = tiles_before + wave_scan_add(tiles), pad_sum = pad_before + wave_scan_add(pad);
-            if (e <= p.E) {
-                starts[e] = g_start;
-                tiles_to[e] = tiles_sum - tiles;
-                pads[e] = pad_sum - pad;
-            }
-            if (e == p.E) {
-                starts[e + 1] = g_end;
-                tiles_to[e + 1] = tiles_sum;
-            }
-            end = at_lane(g_end, 63);
-            tiles_before = at_lane(tiles_sum, 63);
-            pad_before = at_lane(pad_sum, 63);
-        }
-    }
+    if (wave == 0) list_groups(p.offsets, p.E, p.M, TM, starts, tiles_to, pads);
     __syncthreads();
 
     // ---- this workgroup's tiles
@@ -120,12 +97,7 @@ __global__ __launch_bounds__(st::NT) void gemm_fp8_grouped_stream_kernel(Grouped
             pa = reinterpret_cast<uint64_t>(p.A + (int64_t)m0 * lda + pad0);
             pb = reinterpret_cast<uint64_t>(p.B + (int64_t)t.n0 * ldb + pad0);
         } else {
-            int e = 0;      // groups that end at or before tile tm
-            for (int e0 = 0; e0 <= p.E; e0 += 64) {
-                const int l = e0 + (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));      // (no register kept for the lane)
-                e += __popcll(__ballot(l <= p.E && tiles_to[l <= p.E ? l + 1 : 0] <= tm));
-            }
-            e = __builtin_amdgcn_readfirstlane(e);
+            const int e = group_of_tile(tiles_to, p.E, tm);
             t.row = __builtin_amdgcn_readfirstlane(starts[e]) + (tm - __builtin_amdgcn_readfirstlane(tiles_to[e])) * TM;
             t.rows = __builtin_amdgcn_readfirstlane(starts[e + 1]) - t.row;
             if (t.rows > TM) t.rows = TM;
@@ -451,7 +423,7 @@ hipError_t launch_t(const GroupedGemm& g, hipStream_t st) {
     if (cus < NUM_XCD) cus = NUM_XCD;
     const int64_t tiles_m = (g.N + TM - 1) / TM, tiles_n = ((CONTRACT ? g.K : g.N) + BN - 1) / BN;
     const int64_t most = (CONTRACT ? tiles_m * g.E : g.M / TM + (g.E + 1 < g.M ? g.E + 1 : g.M)) * tiles_n;
-    if (most > 0x3FFFFFFF) return hipErrorNotSupported;
+    if (most > 0x3FFFFFFF) return hipErrorInvalidValue;
     int64_t grid = cus / NUM_XCD * NUM_XCD;
     if (const int64_t need = (most + NUM_XCD - 1) / NUM_XCD * NUM_XCD; grid > need) grid = need;
     const GroupedStreamArgs a{g.a, g.lda, g.b, g.ldb, g.scale_a, g.scale_b, g.offsets, (int)g.E, (int)g.M, (int)g.N, (int)g.K,
@@ -470,8 +442,6 @@ hipError_t launch_contract(const GroupedGemm& g, hipStream_t st) {
 }
 
 }  // namespace
-
-bool gemm_fp8_grouped_stream_fits(const GroupedGemm& g) { return g.E <= TABLE_GROUPS && g.ld_out < (1 << 22); }
 
 #define FP8K_FORMATS(CALL)                                                                          \
     if (g.fmt_a == FMT_E4M3FN && g.fmt_b == FMT_E4M3FN) return CALL<FMT_E4M3FN, FMT_E4M3FN>(g, st); \

@@ -131,4 +131,44 @@ __device__ __forceinline__ GroupSpan find_group(const int32_t* __restrict__ offs
     return s;
 }
 
+// The groups' table of a workgroup that walks many tiles, by one wavefront: starts[e] the first row of group e, tiles_to[e] the tiles of
+// `height` rows of the groups before it, pads[e] its place when groups are padded to 128; group E is what lies behind the last one,
+// and entry E + 1 the end.
+__device__ __forceinline__ void list_groups(const int32_t* __restrict__ offsets, int E, int M, int height, int* starts, int* tiles_to, int* pads) {
+    const int lane = threadIdx.x & 63;
+    int end = 0, tiles_before = 0, pad_before = 0;
+    OffsetChunks chunks(offsets, E);
+    for (int e0 = 0; e0 <= E; e0 += 64) {
+        const int e = e0 + lane;
+        int b = chunks.get(e0);
+        if (e >= E) b = e == E ? M : 0;
+        b = b < end ? end : b > M ? M : b;
+        b = wave_scan_max(b);
+        const int a = wave_before(b, end);
+        const int tiles = (b - a + height - 1) / height, pad = (b - a + 127) & ~127;
+        const int tiles_sum = tiles_before + wave_scan_add(tiles), pad_sum = pad_before + wave_scan_add(pad);
+        if (e <= E) {
+            starts[e] = a;
+            tiles_to[e] = tiles_sum - tiles;
+            pads[e] = pad_sum - pad;
+        }
+        if (e == E) {
+            starts[e + 1] = b;
+            tiles_to[e + 1] = tiles_sum;
+        }
+        end = at_lane(b, 63);
+        tiles_before = at_lane(tiles_sum, 63);
+        pad_before = at_lane(pad_sum, 63);
+    }
+}
+// the group of row tile tm, by a whole wavefront: as many groups end at or before it
+__device__ __forceinline__ int group_of_tile(const int* tiles_to, int E, int tm) {
+    int e = 0;
+    for (int e0 = 0; e0 <= E; e0 += 64) {
+        const int l = e0 + (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));      // (no register kept for the lane)
+        e += __popcll(__ballot(l <= E && tiles_to[l <= E ? l + 1 : 0] <= tm));
+    }
+    return __builtin_amdgcn_readfirstlane(e);
+}
+
 }  // namespace fp8k

@@ -37,7 +37,7 @@ bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) %
 bool fmt_ok(int f) { return f == FP8_E4M3FN || f == FP8_E5M2; }
 constexpr int64_t kMaxDim = 0x7FFFFFFF;
 // rows: a grid of one workgroup each counts its threads in 32 bits; leading dimensions: the products' offsets inside a tile are 32 bits
-constexpr int64_t kMaxRows = (1 << 24) - 1, kMaxLd = (1 << 23) - 1;
+constexpr int64_t kMaxRows = (1 << 24) - 1, kMaxLd = (1 << 23) - 1, kMaxCols = (1 << 22) - 128;
 
 size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
@@ -102,9 +102,10 @@ BwdPlan plan_bwd(int64_t M, int64_t E, int64_t K, int64_t N) {
 }
 
 int check_dims(const char* fn, int64_t T, int64_t M, int64_t E, int64_t K, int64_t N, bool bwd) {
-    if (T < 0 || T > kMaxDim || M < 0 || M > kMaxRows || E < 1 || E > kMaxRows || K < 0 || N < 0)
+    if (E < 1 || E > fp8k::GROUPED_MAX_EXPERTS) return fail(FP8_ERR_SHAPE, "%s: E=%lld, 1 .. %d are supported", fn, (ll)E, fp8k::GROUPED_MAX_EXPERTS);
+    if (T < 0 || T > kMaxDim || M < 0 || M > kMaxRows || K < 0 || N < 0)
         return fail(FP8_ERR_SHAPE, "%s: T=%lld M=%lld E=%lld K=%lld N=%lld out of range", fn, (ll)T, (ll)M, (ll)E, (ll)K, (ll)N);
-    if (K > kMaxLd - 127 || N > kMaxLd - 127 || E * K > kMaxDim || E * N > kMaxDim)
+    if (K > kMaxCols || N > kMaxCols || E * K > kMaxDim || E * N > kMaxDim)
         return fail(FP8_ERR_SHAPE, "%s: E=%lld K=%lld N=%lld out of range", fn, (ll)E, (ll)K, (ll)N);
     if (K % 16) return fail(FP8_ERR_SHAPE, "%s: K=%lld must be a multiple of 16", fn, (ll)K);
     if (N % 8) return fail(FP8_ERR_SHAPE, "%s: N=%lld must be a multiple of 8 (dense bfloat16 rows)", fn, (ll)N);

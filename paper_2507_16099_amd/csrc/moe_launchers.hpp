@@ -47,6 +47,7 @@ inline bool grouped_strips(const GroupedColOperand& op, int64_t E) { return op.M
 // columns that the padded groups of M rows can come to
 inline int64_t grouped_padded(int64_t M, int64_t E) { return (M + 127 * (E < M ? E : M) + 127) / 128 * 128; }
 
+constexpr int GROUPED_MAX_EXPERTS = 512;      // the products keep a table of the groups in LDS
 // ---- products grouped by expert (gemm_fp8_grouped.hip): out = A B^T / (scale_a scale_b), operands as for launch_gemm_fp8
 struct GroupedGemm {
     const uint8_t* a; int64_t lda; int fmt_a; const float* scale_a;
@@ -62,8 +63,7 @@ hipError_t launch_grouped_few(const void* x, int64_t T, const int32_t* row_token
 // out[e] [N, K] for each group: A [N, lda], B [K, ldb] with the group's columns where launch_quant_cols_grouped leaves them;
 // scale_a [E, N], scale_b [E, K]
 hipError_t launch_gemm_fp8_grouped_contract(const GroupedGemm& g, hipStream_t st);
-// the same on persistent workgroups with 256 x 256 tiles (gemm_fp8_grouped_stream.hip); _fits: the groups' table has room, 32-bit offsets reach
-bool gemm_fp8_grouped_stream_fits(const GroupedGemm& g);
+// the same with 256 x 256 tiles (gemm_fp8_grouped_stream.hip)
 hipError_t launch_gemm_fp8_grouped_stream_rows(const GroupedGemm& g, hipStream_t st);
 hipError_t launch_gemm_fp8_grouped_stream_contract(const GroupedGemm& g, hipStream_t st);
 
