@@ -324,25 +324,25 @@ hipError_t launch_t(const GroupedGemm& g, hipStream_t st) {
     return hipGetLastError();
 }
 
-// The tile forms: those of RingTile (launchers.hpp) that pay here, one of 32 rows, and the persistent kernel's 256 x 256.
-enum Form { F_32x128 = 0, F_64x64, F_64x128, F_128x128, F_192x128, F_128x256, F_STREAM, FORMS };
+// The tile forms: five of the kernel above, and the 256 x 256 tiles of gemm_fp8_grouped_stream.hip.
+enum Form { F_64x64 = 0, F_64x128, F_128x128, F_192x128, F_128x256, F_STREAM, FORMS };
 // What a form takes, in us: a K step of 128 and the rest of a tile, times the rounds of tiles on the CUs (64 x 64: two tiles a CU), and
 // the bytes at `rate`, whichever is more, as the fourth root of the sum of fourth powers (both count where they are close).  Fitted to 207
-// forwards of 26 shapes (4 .. 128 experts, K and N 512 .. 14400, 1/4 .. 4096 rows an expert on average, groups a factor of 8 apart): off by
-// 11 % in the root mean square, and the form with the least estimate is 5 % behind the best of ten forms on average, 36 % at worst; by
-// the mean number of rows alone (up to 16, 64, 256) 12 % and 86 %.  Others that were tried gain under 0.5 % together: 128 x 64, 96 x 128,
-// 256 x 128.
+// forwards of 26 shapes (4 .. 128 experts, K and N 512 .. 14400, 2 .. 1024 rows an expert on average, groups a factor of 8 apart): off by
+// 10 % in the root mean square, and the form with the least estimate is 4 % behind the best on average, 33 % at worst.  Without 64 x 64 5,
+// without 128 x 256 5, without 256 x 256 6 % on average; 32 x 128 tiles, with a ring of six, gain nothing.
 struct FormCost { int tm, tn, tiles_per_cu; double step, tile; };
-constexpr FormCost kForms[FORMS] = {{32, 128, 1, 0.303, 3.9}, {64, 64, 2, 0.408, 2.9}, {64, 128, 1, 0.382, 3.2}, {128, 128, 1, 0.508, 3.8},
-                                    {192, 128, 1, 0.589, 4.7}, {128, 256, 1, 0.765, 5.6}, {256, 256, 1, 1.151, 7.2}};
+constexpr FormCost kForms[FORMS] = {{64, 64, 2, 0.482, 0.3}, {64, 128, 1, 0.393, 1.0}, {128, 128, 1, 0.514, 1.8}, {192, 128, 1, 0.606, 2.4},
+                                    {128, 256, 1, 0.803, 2.7}, {256, 256, 1, 1.172, 4.8}};
 double form_cost(const FormCost& f, const GroupedGemm& g, int64_t cus) {
     constexpr double rate = 5.1e6;      // bytes a us
     const double busy = g.E < g.M ? (double)g.E : (double)g.M, mean = (double)g.M / (double)g.E;
     // row tiles: groups that have rows have one, longer ones half a tile more than their rows fill
     const double row_tiles = mean < 1 ? busy : busy * std::max(1.0, mean / f.tm + 0.5);
     const double full = row_tiles * (double)((g.N + f.tn - 1) / f.tn) / (double)(cus * f.tiles_per_cu);
-    const double rounds = (std::ceil(0.9 * full) + std::ceil(full) + std::ceil(1.1 * full)) / 3;      // (the number of tiles is an estimate)
-    const double compute = rounds * ((double)((g.K + 127) / 128) * f.step + f.tile);
+    double rounds = (std::ceil(0.9 * full) + std::ceil(full) + std::ceil(1.1 * full)) / 3;      // (the number of tiles is an estimate)
+    if (f.tiles_per_cu == 2 && 2 * full <= 1) rounds = 0.6;      // (a tile that has its CU to itself: one token, 64 experts 1408 x 2048, 64 x 64 11.1 us, 64 x 128 13.0)
+    const double compute = 2.2 + rounds * ((double)((g.K + 127) / 128) * f.step + f.tile);
     const double bytes = (busy * (double)g.K * (double)g.N + (double)g.M * (double)g.K + 2.0 * (double)g.M * (double)g.N) / rate;
     return std::sqrt(std::sqrt(compute * compute * compute * compute + bytes * bytes * bytes * bytes));
 }
@@ -354,7 +354,6 @@ hipError_t launch_form(int form, const GroupedGemm& g, hipStream_t st) {
         case F_64x128: return launch_t<FA, FB, 64, 128, 2, 2, 4, 8, false>(g, st);
         case F_192x128: return launch_t<FA, FB, 192, 128, 2, 2, 3, 4, false>(g, st);
         case F_128x256: return launch_t<FA, FB, 128, 256, 2, 2, 3, 8, false>(g, st);
-        case F_32x128: return launch_t<FA, FB, 32, 128, 1, 4, 6, 1, false>(g, st);
         default: return launch_t<FA, FB, 128, 128, 2, 2, 4, 4, false>(g, st);
     }
 }

@@ -9,8 +9,7 @@
 //
 // A is quantized in place of being read: each wavefront loads its eighth of the rows in the layout of its fragments, the
 // eighths' maxima meet in LDS, scale and codes (those of fp8_quantize) are formed in registers.  The first time this happens behind
-// the first requests of the weight stream, which take as long to arrive; a launch for it, and the wait between the two, was a sixth of a
-// call (see below).  A later row tile waits for its rows with the ring full: 1-2 us of the run.
+// the first requests of the weight stream, which take as long to arrive, instead of in a launch of its own.  A later row tile waits for its rows with the ring full: 1-2 us of the run.
 //
 // Bound: the weights' stream.
 #include "fp8_device.hpp"
@@ -240,22 +239,25 @@ hipError_t launch_t(const FewArgs& a, int64_t grid, hipStream_t st) {
 
 }  // namespace
 
-// Where this form is taken, against quantization and tiles in two launches (us, the other / this, 8 experts 14336 x 4096 with 2, 4, 8, 16
-// rows in all 31.8 28.7 70.3 87.2 / 26.0 26.4 52.7 95.9; 64 experts 1408 x 2048, 2, 8, 32, 64, 128, 256, 512 rows 8.7 9.6 20.0 22.2
-// 35.6 40.9 42.2 / 8.4 13.2 20.7 22.1 30.0 34.3 44.8): up to six rows an expert on average, and one where the weights are large; a K
-// that the eight wavefronts share evenly (2048 x 1408, 64 rows, 21.0 / 35.7; longer ones than 4096, whose rows do not stay in registers
-// between maximum and cast: 4096 x 7168, 2 and 8 rows, 16.8 35.5 / 22.3 46.8); and weights enough that the stream decides.
-static bool few_rows_pay(const GroupedGemm& g) {
+// Where this form is taken, against quantization and tiles in two launches (us, those / this; K shared evenly by the eight wavefronts,
+// and no longer than 4096: longer rows would be read a second time for the cast, 4096 x 7168 with 2 rows 16.8 / 22.3):
+//  * few units of work, where the second launch counts: one token of 8 experts 2048 x 2048, two of them, 11.9 / 9.3; of 128 experts 768 x
+//    2048, eight, 11.1 / 9.7; 4096 x 4096, two of 8, 13.6 / 13.7; beyond: 2048 x 4096, six of 64, 14.3 / 20.4;
+//  * weights enough that the stream decides, and rows few enough that the runs seldom cross: 14336 x 4096, two of 8 experts, 1, 4, 16
+//    tokens 31.0 67.4 89.5 / 25.9 52.0 96.4; 4096 x 4096, two of 16, 8 tokens 45.0 / 35.1; 1408 x 2048, six of 64, 5, 16, 64, 128 tokens
+//    17.2 24.6 37.3 40.7 / 17.8 23.2 35.4 64.0; 768 x 2048, eight of 128, 64 tokens 35.5 / 33.4.
+static bool few_rows_pay(const GroupedGemm& g, int64_t cus) {
     const double busy = (double)(g.E < g.M ? g.E : g.M);
-    const int64_t steps = (g.K + 127) / 128;
-    return g.M <= 6 * g.E && steps % WAVES == 0 && busy * (double)g.N * (double)g.K >= 64e6 && (g.M <= g.E || g.N * g.K <= (int64_t)16 << 20);
+    if ((g.K + 127) / 128 % WAVES != 0) return false;
+    if (g.M * ((g.N + 15) / 16) <= 2 * cus) return true;
+    return g.M <= 6 * g.E && busy * (double)g.N * (double)g.K >= 64e6 && (g.M <= g.E || g.N * g.K <= (int64_t)16 << 20);
 }
 
 // hipErrorNotSupported (nothing launched): more rows, or a longer contraction, than it is for
 hipError_t launch_grouped_few(const void* x, int64_t T, const int32_t* row_token, int fmt_x, int flags, const GroupedGemm& g, hipStream_t st) {
     const int forced = knob(KNOB_SKINNY_DMA);      // 0: never, 2: wherever it fits
-    if (forced == 0 || g.K > 4096 || T < 1 || (forced < 2 && !few_rows_pay(g))) return hipErrorNotSupported;
     const int64_t cus = compute_units() > 0 ? compute_units() : 256;
+    if (forced == 0 || g.K > 4096 || T < 1 || (forced < 2 && !few_rows_pay(g, cus))) return hipErrorNotSupported;
     const int64_t tiles_n = (g.N + 15) / 16, most = (g.M / 16 + (g.E + 1 < g.M ? g.E + 1 : g.M)) * tiles_n;
     if (most > 0x3FFFFFFF) return hipErrorNotSupported;
     int64_t grid = most < cus ? most : cus;

@@ -194,8 +194,8 @@ def load_library() -> C.CDLL:
     L.fp8_internal_set_knob.restype = ci
     L.fp8_internal_set_knob.argtypes = [C.c_char_p, ci]
     # the calls of a served model's layers, which take less time on the GPU than ctypes needs to make them
-    for name in ("quantize", "scaled_mm", "linear_fwd_prequantized", "linear_fwd_prequantized_static", "moe_route", "moe_combine",
-                 "grouped_linear_fwd_prequantized"):
+    for name in ("quantize", "scaled_mm", "linear_fwd_prequantized", "linear_fwd_prequantized_static", "moe_route", "moe_route_bwd",
+                 "moe_combine", "moe_combine_bwd", "grouped_linear_fwd_prequantized"):
         setattr(L, "fast_" + name, _fast(getattr(L, "fp8_" + name)))
     _lib = L
     return L
@@ -784,11 +784,13 @@ def fp8_moe_route_bwd(dgates: torch.Tensor, logits: torch.Tensor, gates: torch.T
     T, E, ld, flags = _logits_of(logits, flags)
     k = gates.shape[1]
     _dense(dgates, (T, k), torch.float32, "dgates"), _dense(gates, (T, k), torch.float32, "gates"), _dense(experts, (T, k), torch.int32, "experts")
+    ld_out = E
     if out is None:
         out = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
-    assert out.shape == (T, E) and out.dtype == logits.dtype
-    _check(load_library().fp8_moe_route_bwd(_ptr(dgates), _ptr(logits), T, E, ld, k, flags, _ptr(gates), _ptr(experts), _ptr(out),
-                                            _mat(out, out.element_size())[2], _stream()))
+    else:
+        assert out.shape == (T, E) and out.dtype == logits.dtype
+        ld_out = _mat(out, out.element_size())[2]
+    _check(load_library().fast_moe_route_bwd(dgates, logits, T, E, ld, k, flags, gates, experts, out, ld_out, _stream()))
     return out
 
 
@@ -799,10 +801,13 @@ def fp8_moe_combine(y: torch.Tensor, gates: torch.Tensor | None, slot_row: torch
     _dense(slot_row, (T, k), torch.int32, "slot_row")
     if gates is not None:
         _dense(gates, (T, k), torch.float32, "gates")
+    ld_out = D
     if out is None:
         out = torch.empty((T, D), dtype=torch.bfloat16, device=y.device)
-    assert out.shape == (T, D)
-    _check(load_library().fast_moe_combine(y, M, ld, gates, slot_row, T, D, k, out, _mat(out, 2)[2], _stream()))
+    else:
+        assert out.shape == (T, D)
+        ld_out = _mat(out, 2)[2]
+    _check(load_library().fast_moe_combine(y, M, ld, gates, slot_row, T, D, k, out, ld_out, _stream()))
     return out
 
 
@@ -828,11 +833,12 @@ def fp8_moe_combine_bwd(dout: torch.Tensor, y: torch.Tensor | None, gates: torch
         assert y is None or not need_dgates or y.shape[0] == M, (y.shape, row_token.shape)
         if dy is None:
             dy = torch.empty((M, D), dtype=torch.bfloat16, device=dout.device)
-        assert dy.shape == (M, D)
-        ld_dy = _mat(dy, 2)[2]
+        else:
+            assert dy.shape == (M, D)
+            ld_dy = _mat(dy, 2)[2]
     dy, dgates = dy if need_dy else None, dgates if need_dgates else None
-    _check(load_library().fp8_moe_combine_bwd(_ptr(dout), ld_dout, _ptr(y) if need_dgates else None, M, ld, _ptr(gates), _ptr(slot_row),
-                                              _ptr(row_token) if need_dy else None, T, D, k, _ptr(dy), ld_dy, _ptr(dgates), _stream()))
+    _check(load_library().fast_moe_combine_bwd(dout, ld_dout, y if need_dgates else None, M, ld, gates, slot_row, row_token if need_dy else None,
+                                               T, D, k, dy, ld_dy, dgates, _stream()))
     return dy, dgates
 
 
