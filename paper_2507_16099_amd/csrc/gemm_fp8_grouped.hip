@@ -324,16 +324,16 @@ hipError_t launch_t(const GroupedGemm& g, hipStream_t st) {
     return hipGetLastError();
 }
 
-// The tile forms: five of the kernel above, and the 256 x 256 tiles of gemm_fp8_grouped_stream.hip.
-enum Form { F_64x64 = 0, F_64x128, F_128x128, F_192x128, F_128x256, F_STREAM, FORMS };
+// The tile forms: four of the kernel above, and those of gemm_fp8_grouped_stream.hip.
+enum Form { F_64x64 = 0, F_64x128, F_128x128, F_128x256, F_192x256, F_256x256, FORMS };
 // What a form takes, in us: a K step of 128 and the rest of a tile, times the rounds of tiles on the CUs (64 x 64: two tiles a CU), and
 // the bytes at `rate`, whichever is more, as the fourth root of the sum of fourth powers (both count where they are close).  Fitted to 207
 // forwards of 26 shapes (4 .. 128 experts, K and N 512 .. 14400, 2 .. 1024 rows an expert on average, groups a factor of 8 apart): off by
-// 10 % in the root mean square, and the form with the least estimate is 4 % behind the best on average, 33 % at worst.  Without 64 x 64 5,
-// without 128 x 256 5, without 256 x 256 6 % on average; 32 x 128 tiles, with a ring of six, gain nothing.
+// 9 % in the root mean square, and the form with the least estimate is 3.6 % behind the best on average, 34 % at worst.  Without 64 x 64 4.5,
+// without 128 x 256 4.3, without 256 x 256 5.1 % on average; 192 x 128 tiles give 0.1, 32 x 128, with a ring of six, nothing.
 struct FormCost { int tm, tn, tiles_per_cu; double step, tile; };
-constexpr FormCost kForms[FORMS] = {{64, 64, 2, 0.482, 0.3}, {64, 128, 1, 0.393, 1.0}, {128, 128, 1, 0.514, 1.8}, {192, 128, 1, 0.606, 2.4},
-                                    {128, 256, 1, 0.803, 2.7}, {256, 256, 1, 1.172, 4.8}};
+constexpr FormCost kForms[FORMS] = {{64, 64, 2, 0.474, 0.3}, {64, 128, 1, 0.385, 1.0}, {128, 128, 1, 0.501, 1.8},
+                                    {128, 256, 1, 0.787, 2.6}, {192, 256, 1, 0.956, 3.1}, {256, 256, 1, 1.101, 4.4}};
 double form_cost(const FormCost& f, const GroupedGemm& g, int64_t cus) {
     constexpr double rate = 5.1e6;      // bytes a us
     const double busy = g.E < g.M ? (double)g.E : (double)g.M, mean = (double)g.M / (double)g.E;
@@ -342,7 +342,7 @@ double form_cost(const FormCost& f, const GroupedGemm& g, int64_t cus) {
     const double full = row_tiles * (double)((g.N + f.tn - 1) / f.tn) / (double)(cus * f.tiles_per_cu);
     double rounds = (std::ceil(0.9 * full) + std::ceil(full) + std::ceil(1.1 * full)) / 3;      // (the number of tiles is an estimate)
     if (f.tiles_per_cu == 2 && 2 * full <= 1) rounds = 0.6;      // (a tile that has its CU to itself: one token, 64 experts 1408 x 2048, 64 x 64 11.1 us, 64 x 128 13.0)
-    const double compute = 2.2 + rounds * ((double)((g.K + 127) / 128) * f.step + f.tile);
+    const double compute = 1.0 + rounds * ((double)((g.K + 127) / 128) * f.step + f.tile);
     const double bytes = (busy * (double)g.K * (double)g.N + (double)g.M * (double)g.K + 2.0 * (double)g.M * (double)g.N) / rate;
     return std::sqrt(std::sqrt(compute * compute * compute * compute + bytes * bytes * bytes * bytes));
 }
@@ -352,7 +352,6 @@ hipError_t launch_form(int form, const GroupedGemm& g, hipStream_t st) {
     switch (form) {
         case F_64x64: return launch_t<FA, FB, 64, 64, 2, 2, 4, 4, false>(g, st);
         case F_64x128: return launch_t<FA, FB, 64, 128, 2, 2, 4, 8, false>(g, st);
-        case F_192x128: return launch_t<FA, FB, 192, 128, 2, 2, 3, 4, false>(g, st);
         case F_128x256: return launch_t<FA, FB, 128, 256, 2, 2, 3, 8, false>(g, st);
         default: return launch_t<FA, FB, 128, 128, 2, 2, 4, 4, false>(g, st);
     }
@@ -360,18 +359,17 @@ hipError_t launch_form(int form, const GroupedGemm& g, hipStream_t st) {
 
 template <int FA, int FB>
 hipError_t launch_rows(const GroupedGemm& g, hipStream_t st) {
-    const int forced = knob(KNOB_GEMM_RING), stream = knob(KNOB_GEMM_STREAM);      // 1 + form; 0: never, 2: wherever it fits
-    int form = 0;
-    if (forced > 0) {
-        form = forced - 1 < F_STREAM ? forced - 1 : F_128x128;
-    } else {
+    // the switches: 1 + form; the forms of the other file 0: never, 2: always the best of them
+    const int forced = knob(KNOB_GEMM_RING), stream = knob(KNOB_GEMM_STREAM);
+    int form = forced - 1;
+    if (forced <= 0 || forced > FORMS) {
         const int64_t cus = compute_units() > 0 ? compute_units() : 256;
-        const bool fits = stream != 0;
-        for (int f = 1; f < (fits ? FORMS : F_STREAM); ++f)
+        const int first = stream >= 2 ? F_192x256 : 0, end = stream == 0 ? F_192x256 : FORMS;
+        form = first;
+        for (int f = first + 1; f < end; ++f)
             if (form_cost(kForms[f], g, cus) < form_cost(kForms[form], g, cus)) form = f;
-        if (fits && stream >= 2) form = F_STREAM;
     }
-    if (form == F_STREAM) return launch_gemm_fp8_grouped_stream_rows(g, st);
+    if (form >= F_192x256) return launch_gemm_fp8_grouped_stream_rows(g, kForms[form].tm, st);
     return launch_form<FA, FB>(form, g, st);
 }
 

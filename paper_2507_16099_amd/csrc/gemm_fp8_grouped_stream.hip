@@ -433,7 +433,9 @@ hipError_t launch_t(const GroupedGemm& g, hipStream_t st) {
 }
 
 template <int FA, int FB>
-hipError_t launch_rows(const GroupedGemm& g, hipStream_t st) { return launch_t<FA, FB, 4, false>(g, st); }
+hipError_t launch_rows(const GroupedGemm& g, int height, hipStream_t st) {
+    return height == 192 ? launch_t<FA, FB, 2, false>(g, st) : launch_t<FA, FB, 4, false>(g, st);
+}
 template <int FA, int FB>
 hipError_t launch_contract(const GroupedGemm& g, hipStream_t st) {
     if (g.M <= 192 * g.E) return launch_t<FA, FB, 2, true, true>(g, st);
@@ -443,13 +445,13 @@ hipError_t launch_contract(const GroupedGemm& g, hipStream_t st) {
 
 }  // namespace
 
-#define FP8K_FORMATS(CALL)                                                                          \
-    if (g.fmt_a == FMT_E4M3FN && g.fmt_b == FMT_E4M3FN) return CALL<FMT_E4M3FN, FMT_E4M3FN>(g, st); \
-    if (g.fmt_a == FMT_E5M2 && g.fmt_b == FMT_E4M3FN) return CALL<FMT_E5M2, FMT_E4M3FN>(g, st);     \
-    if (g.fmt_a == FMT_E4M3FN) return CALL<FMT_E4M3FN, FMT_E5M2>(g, st);                            \
-    return CALL<FMT_E5M2, FMT_E5M2>(g, st);
+#define FP8K_FORMATS(CALL, ...)                                                                                 \
+    if (g.fmt_a == FMT_E4M3FN && g.fmt_b == FMT_E4M3FN) return CALL<FMT_E4M3FN, FMT_E4M3FN>(g, __VA_ARGS__); \
+    if (g.fmt_a == FMT_E5M2 && g.fmt_b == FMT_E4M3FN) return CALL<FMT_E5M2, FMT_E4M3FN>(g, __VA_ARGS__);     \
+    if (g.fmt_a == FMT_E4M3FN) return CALL<FMT_E4M3FN, FMT_E5M2>(g, __VA_ARGS__);                            \
+    return CALL<FMT_E5M2, FMT_E5M2>(g, __VA_ARGS__);
 
-hipError_t launch_gemm_fp8_grouped_stream_rows(const GroupedGemm& g, hipStream_t st) { FP8K_FORMATS(launch_rows) }
-hipError_t launch_gemm_fp8_grouped_stream_contract(const GroupedGemm& g, hipStream_t st) { FP8K_FORMATS(launch_contract) }
+hipError_t launch_gemm_fp8_grouped_stream_rows(const GroupedGemm& g, int height, hipStream_t st) { FP8K_FORMATS(launch_rows, height, st) }
+hipError_t launch_gemm_fp8_grouped_stream_contract(const GroupedGemm& g, hipStream_t st) { FP8K_FORMATS(launch_contract, st) }
 
 }  // namespace fp8k

@@ -63,8 +63,8 @@ hipError_t launch_grouped_few(const void* x, int64_t T, const int32_t* row_token
 // out[e] [N, K] for each group: A [N, lda], B [K, ldb] with the group's columns where launch_quant_cols_grouped leaves them;
 // scale_a [E, N], scale_b [E, K]
 hipError_t launch_gemm_fp8_grouped_contract(const GroupedGemm& g, hipStream_t st);
-// the same with 256 x 256 tiles (gemm_fp8_grouped_stream.hip)
-hipError_t launch_gemm_fp8_grouped_stream_rows(const GroupedGemm& g, hipStream_t st);
+// the same with tiles of 256 (rows: or 192) x 256 (gemm_fp8_grouped_stream.hip)
+hipError_t launch_gemm_fp8_grouped_stream_rows(const GroupedGemm& g, int height, hipStream_t st);
 hipError_t launch_gemm_fp8_grouped_stream_contract(const GroupedGemm& g, hipStream_t st);
 
 // ---- AdamW (adamw.hip)

@@ -38,6 +38,9 @@ def test_route(T, E, k, renorm, dtype):
     wide = torch.full((T, E + 3), 9.0, dtype=dtype)      # rows further apart than they are long
     wide[:, :E] = x
     flags = fp8.FP8_ROUTE_RENORM if renorm else 0
+    dgates = torch.randn((T, k), generator=_gen(5)).cuda()
+    dg = dgates.cpu().double().numpy()
+    full = ref.route_bwd(x, dg, want["gates"], want["experts"], renorm)
     for logits in (x.cuda(), wide.cuda()[:, :E]):
         gates, experts, offsets, row_token, slot_row = fp8.fp8_moe_route(logits, k, flags)
         for name, got in (("experts", experts), ("offsets", offsets), ("row_token", row_token), ("slot_row", slot_row)):
@@ -45,10 +48,7 @@ def test_route(T, E, k, renorm, dtype):
         # exponents: the difference's rounding (at most 20 here) and the function's own few; E terms in the sum, a division
         got = gates.cpu().double().numpy()
         assert (np.abs(got - want["gates"]) <= (20 + 8 + E) * 2.0 ** -24 * want["gates"]).all()
-        dgates = torch.randn((T, k), generator=_gen(5)).cuda()
         d = fp8.fp8_moe_route_bwd(dgates, logits, gates, experts, flags)
-        dg = dgates.cpu().double().numpy()
-        full = ref.route_bwd(x, dg, want["gates"], want["experts"], renorm)
         size = np.abs(dg).sum(1, keepdims=True) + 1e-30      # no entry's terms are larger
         step = 2.0 ** -8 if dtype == BF16 else 2.0 ** -24
         assert (np.abs(d.cpu().double().numpy() - full) <= step * np.abs(full) + (3 * (28 + E) + k + 4) * 2.0 ** -24 * size).all()
@@ -229,7 +229,7 @@ def test_few_rows_against_quantized_weights(case, recipe):
                                             row_token=row_token.cuda(), y=y)
     ref.assert_product(y.cpu(), want, size)
     # every form that takes such a call: quantization inside the product, tiles of every size, persistent workgroups
-    for switches in ({"SKINNY_DMA": 2}, *({"SKINNY_DMA": 0, "GEMM_RING": 1 + f} for f in range(6)), {"SKINNY_DMA": 0, "GEMM_STREAM": 2},
+    for switches in ({"SKINNY_DMA": 2}, *({"SKINNY_DMA": 0, "GEMM_RING": 1 + f} for f in range(6)),
                      {"SKINNY_DMA": 0, "GEMM_STREAM": 8}):
         with knobs(**switches):
             other = torch.full_like(y, float("nan"))
@@ -251,7 +251,8 @@ def test_every_form_of_the_products(case):
     want, size = ref.grouped_fwd(xr, w, offsets, ref.E4M3, ref.E4M3, False)
     (want_dx, size_dx), (want_dw, size_dw) = ref.grouped_bwd(dy, xr, w, offsets, ref.E5M2, ref.E4M3, ref.E4M3, False)
     args = (x.cuda(), w.cuda(), offsets.cuda(), r)
-    for switches in (*({"GEMM_RING": 1 + f, "GEMM_STREAM": 0} for f in range(6)), {"GEMM_STREAM": 2}, {"GEMM_STREAM": 8}):
+    for switches in (*({"GEMM_RING": 1 + f} for f in range(6)), {"GEMM_RING": 5, "GEMM_STREAM": 8}, {"GEMM_RING": 6, "GEMM_STREAM": 8},
+                     {"GEMM_RING": 3, "GEMM_STREAM": 8}, {"GEMM_RING": 4, "GEMM_STREAM": 0}):
         with knobs(**switches):
             y = fp8.fp8_grouped_linear_fwd(*args, row_token=row_token.cuda())
             dx, dw = fp8.fp8_grouped_linear_bwd(dy.cuda(), *args, row_token=row_token.cuda())
