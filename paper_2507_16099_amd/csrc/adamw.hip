@@ -10,9 +10,9 @@
 // zero is never stored as zero (it would leave m / eps): it becomes the smallest code.  The update of this step uses m and v from before
 // the rounding.
 //
-// One launch, however many tensors: the caller keeps a table of them in device memory, which also says for each workgroup which piece
-// of which tensor it has (a search through the sizes would be a chain of loads).  Pieces are 2048 elements, one trip of a
-// workgroup, or where that makes more workgroups than PLENTY, 8192.
+// One launch, however many tensors: the caller keeps a table in device memory that has each workgroup's piece of a tensor ready, so that one load
+// leads to the data (a search through the sizes, or a list of pieces that names tensors, is a chain of them).  Pieces are 2048
+// elements, one trip of a workgroup, or where that makes more workgroups than PLENTY, 8192.
 // Bound: HBM, 10 bytes an element (bfloat16, 8-bit moments) to 28 (all binary32).
 #include "fp8_device.hpp"
 #include "moe_launchers.hpp"
@@ -137,19 +137,16 @@ __device__ __forceinline__ float inverse_pow2(float s) { return __uint_as_float(
 // a thread: eight elements at a time; 32 lanes hold a block of 256
 template <class P, class G, bool FP8>
 __global__ __launch_bounds__(NT) void adamw_kernel(const AdamwHeader* __restrict__ table, int flags, AdamwScalars s) {
-    const AdamwTensor* tensors = reinterpret_cast<const AdamwTensor*>(table + 1);
-    const int64_t count = table->count;
-    // (a table made for other types, or for fewer workgroups, changes nothing)
-    if (table->flags != flags || (int64_t)blockIdx.x >= table->blocks) return;
-    const AdamwBlock b = reinterpret_cast<const AdamwBlock*>(tensors + count)[blockIdx.x];
-    const AdamwTensor t = tensors[b.tensor];
-    const int rounds = table->rounds;
-    const int64_t i0 = (int64_t)b.piece * rounds * TRIP;
+    // (requested together; a table made for other types, or for fewer workgroups, changes nothing)
+    const AdamwPiece t = reinterpret_cast<const AdamwPiece*>(table + 1)[blockIdx.x];
+    const int64_t blocks = table->blocks;
+    const int made_for = table->flags, rounds = table->rounds;
+    if (made_for != flags || (int64_t)blockIdx.x >= blocks) return;
     const Update u{s, s.grad_scale ? *s.grad_scale : 1.0f};
     P* p = static_cast<P*>(t.p);
     const G* g = static_cast<const G*>(t.g);
     for (int r = 0; r < rounds; ++r) {
-        const int64_t i = i0 + (int64_t)(r * NT + (int)threadIdx.x) * 8;
+        const int64_t i = (int64_t)(r * NT + (int)threadIdx.x) * 8;
         const int64_t left = t.n - i;
         const int n = left >= 8 ? 8 : left > 0 ? (int)left : 0;
         if (!FP8 && n == 0) return;
@@ -210,7 +207,7 @@ int64_t pieces(int64_t n, int rounds) { return (n + (int64_t)rounds * TRIP - 1) 
 }  // namespace
 
 AdamwHeader adamw_header(const AdamwTensor* tensors, int64_t count, int flags) {
-    AdamwHeader h{count, 0, flags, 1, 0};
+    AdamwHeader h{0, flags, 1, {}};
     for (int64_t i = 0; i < count; ++i) h.blocks += pieces(tensors[i].n, 1);
     if (h.blocks > PLENTY) {
         h.rounds = 4;
@@ -221,16 +218,19 @@ AdamwHeader adamw_header(const AdamwTensor* tensors, int64_t count, int flags) {
     return h;
 }
 
-void adamw_fill_table(const AdamwTensor* tensors, const AdamwHeader& h, void* table) {
+void adamw_fill_table(const AdamwTensor* tensors, int64_t count, const AdamwHeader& h, void* table) {
     char* at = static_cast<char*>(table);
     std::memcpy(at, &h, sizeof(h));
     at += sizeof(h);
-    for (int64_t i = 0; i < h.count; ++i, at += sizeof(AdamwTensor)) std::memcpy(at, &tensors[i], sizeof(AdamwTensor));
-    for (int64_t i = 0; i < h.count; ++i) {
-        const int64_t n = pieces(tensors[i].n, h.rounds);
-        for (int64_t j = 0; j < n; ++j, at += sizeof(AdamwBlock)) {
-            const AdamwBlock b{(int32_t)i, (int32_t)j};
-            std::memcpy(at, &b, sizeof(b));
+    const bool p_f32 = h.flags & ADAMW_PARAM_FP32, g_f32 = h.flags & ADAMW_GRAD_FP32, q = h.flags & ADAMW_STATE_FP8;
+    const int64_t size = (int64_t)h.rounds * TRIP;
+    for (int64_t i = 0; i < count; ++i) {
+        const AdamwTensor& t = tensors[i];
+        for (int64_t d = 0; d < t.n; d += size, at += sizeof(AdamwPiece)) {
+            const AdamwPiece piece{static_cast<char*>(t.p) + d * (p_f32 ? 4 : 2), static_cast<const char*>(t.g) + d * (g_f32 ? 4 : 2),
+                                   static_cast<char*>(t.m) + d * (q ? 1 : 4), static_cast<char*>(t.v) + d * (q ? 1 : 4),
+                                   q ? t.sm + d / 256 : nullptr, q ? t.sv + d / 256 : nullptr, t.n - d < size ? t.n - d : size, 0};
+            std::memcpy(at, &piece, sizeof(piece));
         }
     }
 }

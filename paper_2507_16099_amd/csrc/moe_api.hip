@@ -358,6 +358,7 @@ int fp8_grouped_linear_fwd_prequantized(const void* x, int64_t T, const int32_t*
 }
 
 static_assert(sizeof(fp8_adamw_tensor) == sizeof(fp8k::AdamwTensor), "the same layout");
+static_assert(fp8k::ADAMW_PARAM_FP32 == FP8_ADAMW_PARAM_FP32 && fp8k::ADAMW_GRAD_FP32 == FP8_ADAMW_GRAD_FP32 && fp8k::ADAMW_STATE_FP8 == FP8_ADAMW_STATE_FP8, "flags");
 static const fp8k::AdamwTensor* as_internal(const fp8_adamw_tensor* t) { return reinterpret_cast<const fp8k::AdamwTensor*>(t); }
 
 constexpr int kAdamwFlags = FP8_ADAMW_PARAM_FP32 | FP8_ADAMW_GRAD_FP32 | FP8_ADAMW_STATE_FP8;
@@ -396,7 +397,7 @@ int fp8_adamw_table(const fp8_adamw_tensor* tensors, int64_t count, int flags, v
     const fp8k::AdamwHeader h = fp8k::adamw_header(as_internal(tensors), count, flags);
     const size_t want = fp8k::adamw_table_bytes(h);
     if (table_bytes < want) return fail(FP8_ERR_WORKSPACE, "%s: table %zu < %zu bytes", fn, table_bytes, want);
-    fp8k::adamw_fill_table(as_internal(tensors), h, table);
+    fp8k::adamw_fill_table(as_internal(tensors), count, h, table);
     *blocks = h.blocks;
     return FP8_OK;
 }

@@ -69,13 +69,15 @@ hipError_t launch_gemm_fp8_grouped_stream_contract(const GroupedGemm& g, hipStre
 
 // ---- AdamW (adamw.hip)
 struct AdamwTensor { void* p; const void* g; void *m, *v; float *sm, *sv; int64_t n; };
+constexpr int ADAMW_PARAM_FP32 = 256, ADAMW_GRAD_FP32 = 512, ADAMW_STATE_FP8 = 1024;      // of the ABI's flags
 struct AdamwScalars { float b1, c1, b2, c2, decay, rate, inv_root, eps; const float* grad_scale; };
-// The table in device memory that a step reads: a header, the tensors, and for each workgroup which piece of which tensor it has.
-struct AdamwHeader { int64_t count, blocks; int32_t flags, rounds; int64_t reserved; };
-struct AdamwBlock { int32_t tensor, piece; };
+// The table in device memory that a step reads: a header, and for each workgroup its piece of a tensor, all pointers moved to it.
+struct AdamwHeader { int64_t blocks; int32_t flags, rounds; int64_t reserved[6]; };
+struct AdamwPiece { void* p; const void* g; void *m, *v; float *sm, *sv; int64_t n, reserved; };
+static_assert(sizeof(AdamwHeader) == 64 && sizeof(AdamwPiece) == 64, "whole pieces of a cache line");
 AdamwHeader adamw_header(const AdamwTensor* tensors, int64_t count, int flags);      // blocks < 0: too many
-inline size_t adamw_table_bytes(const AdamwHeader& h) { return sizeof(AdamwHeader) + (size_t)h.count * sizeof(AdamwTensor) + (size_t)h.blocks * sizeof(AdamwBlock); }
-void adamw_fill_table(const AdamwTensor* tensors, const AdamwHeader& h, void* table);
+inline size_t adamw_table_bytes(const AdamwHeader& h) { return sizeof(AdamwHeader) + (size_t)h.blocks * sizeof(AdamwPiece); }
+void adamw_fill_table(const AdamwTensor* tensors, int64_t count, const AdamwHeader& h, void* table);
 hipError_t launch_adamw(const void* table, int64_t blocks, int flags, bool p_f32, bool g_f32, bool fp8_state, const AdamwScalars& s, hipStream_t st);
 
 }  // namespace fp8k
