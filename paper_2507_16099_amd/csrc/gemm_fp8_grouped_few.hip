@@ -9,7 +9,8 @@
 //
 // A is quantized in place of being read: each wavefront loads its eighth of the rows in the layout of its fragments, the
 // eighths' maxima meet in LDS, scale and codes (those of fp8_quantize) are formed in registers.  The first time this happens behind
-// the first requests of the weight stream, which take as long to arrive, instead of in a launch of its own.  A later row tile waits for its rows with the ring full: 1-2 us of the run.
+// the first requests of the weight stream, which take as long to arrive, instead of in a launch of its own.  A later row tile waits for
+// its rows with the ring full: 1-2 us of the run.
 //
 // Bound: the weights' stream.
 #include "fp8_device.hpp"

@@ -100,12 +100,12 @@ __device__ __forceinline__ GroupTile find_group_tile(const int32_t* __restrict__
     return t;
 }
 
-// the rows of one group, and where it lies in the padded order
-struct GroupSpan { int row0, rows, pad0; };
-__device__ __forceinline__ GroupSpan find_group(const int32_t* __restrict__ offsets, int E, int M, int group) {
+// the rows of one group, where it lies in the padded order, and how many tiles of `height` rows the groups before it have
+struct GroupSpan { int row0, rows, pad0, tile0; };
+__device__ __forceinline__ GroupSpan find_group(const int32_t* __restrict__ offsets, int E, int M, int group, int height) {
     const int lane = threadIdx.x & 63;
-    GroupSpan s{0, 0, 0};
-    int end = 0, pad_before = 0;
+    GroupSpan s{0, 0, 0, 0};
+    int end = 0, pad_before = 0, tiles_before = 0;
     OffsetChunks chunks(offsets, E);
     for (int e0 = 0; e0 <= group; e0 += 64) {
         const int e = e0 + lane;
@@ -114,20 +114,19 @@ __device__ __forceinline__ GroupSpan find_group(const int32_t* __restrict__ offs
         b = b < end ? end : b > M ? M : b;
         b = wave_scan_max(b);
         const int a = wave_before(b, end);
-        const int pad = (b - a + 127) & ~127;
-        const int pad_to = pad_before + wave_scan_add(pad);
+        const int pad = (b - a + 127) & ~127, tiles = (b - a + height - 1) / height;
+        const int pad_to = pad_before + wave_scan_add(pad), tiles_to = tiles_before + wave_scan_add(tiles);
         if (group < e0 + 64) {
             const int l = group - e0;
             s.row0 = at_lane(a, l);
             s.rows = at_lane(b - a, l);
             s.pad0 = at_lane(pad_to, l) - at_lane(pad, l);
+            s.tile0 = at_lane(tiles_to, l) - at_lane(tiles, l);
         }
         end = at_lane(b, 63);
         pad_before = at_lane(pad_to, 63);
+        tiles_before = at_lane(tiles_to, 63);
     }
-    s.row0 = __builtin_amdgcn_readfirstlane(s.row0);
-    s.rows = __builtin_amdgcn_readfirstlane(s.rows);
-    s.pad0 = __builtin_amdgcn_readfirstlane(s.pad0);
     return s;
 }
 

@@ -10,6 +10,7 @@
 #include "fp8_device.hpp"
 #include "group_tiles.hpp"
 #include "moe_launchers.hpp"
+#include "tuning.hpp"
 
 namespace fp8k {
 
@@ -167,6 +168,96 @@ __global__ __launch_bounds__(256) void cols_amax_kernel(ColArgs a) {
     }
 }
 
+// Rows and maxima from one read, for the gradient of long groups: a workgroup takes `height` rows of a group one by one, writes their codes and
+// scales and keeps its columns' maxima, eight a thread and piece; at its end they go to a matrix of maxima per tile, which lies in the
+// output of the cast and is folded per group ahead of it.  The next row is under way while one is cast.
+// The height is what fills the CUs with whole rounds of workgroups: 16384 rows x 14336 in eight groups, two workgroups a CU, 32 rows (520
+// tiles, a second round for eight of them) 168 us, 33 rows 143 and 5.7 for the fold; rows alone and maxima alone 114 + 85.  (Atomic
+// maxima per tile in place of the matrix: 225 us with 64 rows a tile, 243 with 32.)  The cast behind it finds more of the operand in
+// the last-level cache: 125 us, behind the maxima alone 139.
+template <int FMT, int NV>
+__global__ __launch_bounds__(512) void rows_cols_amax_kernel(ColArgs a, uint8_t* __restrict__ q, int64_t ld_q, float* __restrict__ scale,
+                                                              int height) {
+    constexpr int NTH = 512;
+    __shared__ uint32_t part[2][NTH / 64];
+    const GroupTile t = find_group_tile<true>(a.offsets, a.E, a.M, height, blockIdx.x);
+    if (t.group < 0) return;
+    const int tid = threadIdx.x;
+    const bool in_group = t.group < a.E;      // (rows behind the last group have codes too, and no column)
+    uint4 v[NV], next[NV], m[NV];
+    auto fetch = [&](int r, uint4 (&to)[NV]) {
+        const uint16_t* row = a.x + (int64_t)(t.row0 + r) * a.ldx;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * NTH + tid) * 8;
+            to[i] = c < a.cols ? *reinterpret_cast<const uint4*>(row + c) : make_uint4(0, 0, 0, 0);
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < NV; ++i) m[i] = make_uint4(0, 0, 0, 0);
+    // (tiles start `height` rows apart, which can be a multiple of 4096 bytes: each begins at another of its rows)
+    int r = (int)blockIdx.x % t.rows;
+    fetch(r, next);
+    for (int n = 0; n < t.rows; ++n) {
+        const int r_next = r + 1 < t.rows ? r + 1 : 0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] = next[i];
+        if (n + 1 < t.rows) fetch(r_next, next);
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            top = pk_absmax4(top, v[i]);
+            m[i].x = pk_absmax(m[i].x, v[i].x); m[i].y = pk_absmax(m[i].y, v[i].y);
+            m[i].z = pk_absmax(m[i].z, v[i].z); m[i].w = pk_absmax(m[i].w, v[i].w);
+        }
+        top = wave_max_u32<64>(pk_fold(top));
+        if ((tid & 63) == 0) part[n & 1][tid >> 6] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < NTH / 64; ++w) top = part[n & 1][w] > top ? part[n & 1][w] : top;
+        const float s = scale_from_amax(mag_to_float(top), FMT, a.flags);
+        if (tid == 0) scale[t.row0 + r] = s;
+        uint8_t* out = q + (int64_t)(t.row0 + r) * ld_q;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * NTH + tid) * 8;
+            if (c < a.cols) store_vec(out + c, s < CLAMP_FROM ? cast8_own<FMT, false>(v[i], s) : cast8_own<FMT, true>(v[i], s), a.keep);
+        }
+        r = r_next;
+    }
+    if (!in_group) return;
+    uint16_t* const to = reinterpret_cast<uint16_t*>(a.qt) + (int64_t)blockIdx.x * a.cols;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * NTH + tid) * 8;
+        if (c < a.cols) *reinterpret_cast<uint4*>(to + c) = m[i];
+    }
+}
+// maxima of a group's tiles -> maxima of the group: 512 columns a workgroup, a wavefront every fourth tile
+__global__ __launch_bounds__(256) void fold_tiles_kernel(ColArgs a, int height) {
+    __shared__ uint4 part[4][64];
+    const GroupSpan s = find_group(a.offsets, a.E, a.M, blockIdx.y, height);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tiles = (s.rows + height - 1) / height;
+    const int c = (int)blockIdx.x * 512 + lane * 8;
+    const uint16_t* from = reinterpret_cast<const uint16_t*>(a.qt) + (int64_t)s.tile0 * a.cols + c;
+    uint4 m = make_uint4(0, 0, 0, 0);
+    if (c < a.cols) {
+#pragma unroll 8
+        for (int t = wave; t < tiles; t += 4) {
+            const uint4 v = *reinterpret_cast<const uint4*>(from + (int64_t)t * a.cols);
+            m.x = pk_absmax(m.x, v.x); m.y = pk_absmax(m.y, v.y);
+            m.z = pk_absmax(m.z, v.z); m.w = pk_absmax(m.w, v.w);
+        }
+    }
+    part[wave][lane] = m;
+    __syncthreads();
+    const int l = threadIdx.x >> 2, d = threadIdx.x & 3, col = (int)blockIdx.x * 512 + l * 8 + d * 2;
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w = pk_absmax(w, reinterpret_cast<const uint32_t*>(&part[i][l])[d]);
+    if (col < a.cols) *reinterpret_cast<uint2*>(a.amax + (int64_t)blockIdx.y * a.cols + col) = make_uint2(w & 0xFFFFu, w >> 16);
+}
+
 // Cast: 128 rows x 128 columns.  Thread (p, l) = (tid / 16, tid % 16) holds rows 4 p .. 4 p + 3 and 64 + those, eight columns from
 // 8 l on; four rows turn into a dword of codes per column.  In LDS a column is 128 bytes, its sixteen-byte pieces exchanged by
 // (column / 8) % 8, so that the sixteen lanes that write the same rows of sixteen columns eight apart meet in two of them at most.
@@ -253,7 +344,7 @@ __device__ __forceinline__ void strip(const ColArgs& a, int block, uint8_t* turn
     int row0, rows;
     int64_t out0;      // where the group's codes start
     if (a.offsets) {
-        const GroupSpan s = find_group(a.offsets, a.E, a.M, e);
+        const GroupSpan s = find_group(a.offsets, a.E, a.M, e, 128);
         row0 = s.row0;
         rows = s.rows;
         out0 = s.pad0;
@@ -387,7 +478,8 @@ hipError_t launch_quant_rows_gather(const void* x, int64_t T, int64_t ldx, const
 }
 
 static ColArgs col_args(const GroupedColOperand& op, const int32_t* offsets, int64_t E, int flags) {
-    return ColArgs{static_cast<const uint16_t*>(op.x), op.T, op.ldx, op.row_token, op.uniform ? nullptr : offsets, (int)op.M, (int)E, (int)op.cols, flags, op.M * op.cols <= (int64_t)64 << 20,
+    return ColArgs{static_cast<const uint16_t*>(op.x), op.T, op.ldx, op.row_token, op.uniform ? nullptr : offsets, (int)op.M, (int)E, (int)op.cols, flags,
+                  op.M * op.cols <= (int64_t)64 << 20,
                    op.qt, op.ld_t, op.uniform ? op.cols * op.ld_t : 0, 0, op.scale, op.amax};
 }
 
@@ -425,19 +517,54 @@ hipError_t launch_quant_strips_grouped(const GroupedColOperand& op, const Groupe
     return launch(32, strips_kernel<512, 4, 5>, 512);
 }
 
-hipError_t launch_quant_cols_grouped(const GroupedColOperand& op, const int32_t* offsets, int64_t E, int flags, hipStream_t st) {
-    if (op.M <= 0) return hipSuccess;
-    ColArgs a = col_args(op, offsets, E, flags);
-    // tiles of 128 rows: what the groups can come to at most
-    const int64_t tiles = a.offsets ? op.M / 128 + (E < op.M ? E : op.M) : E * ((op.M / E + 127) / 128);
-    if (tiles * ((op.cols + 127) / 128) >= 1 << 24) return hipErrorInvalidValue;
-    a.tiles = (int)tiles;
-    cols_amax_kernel<<<xcd_grid(tiles * ((op.cols + 511) / 512)), 256, 0, st>>>(a);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    const unsigned grid = xcd_grid(tiles * ((op.cols + 127) / 128));
+// tiles of 128 rows of the operand: what the groups can come to at most
+static hipError_t cast_cols(const GroupedColOperand& op, const ColArgs& a, hipStream_t st) {
+    const unsigned grid = xcd_grid((int64_t)a.tiles * ((op.cols + 127) / 128));
     if (op.fmt == FMT_E4M3FN) cols_cast_kernel<FMT_E4M3FN><<<grid, 256, 0, st>>>(a);
     else cols_cast_kernel<FMT_E5M2><<<grid, 256, 0, st>>>(a);
     return hipGetLastError();
+}
+static bool with_tiles(const GroupedColOperand& op, int64_t E, ColArgs& a) {
+    const int64_t tiles = a.offsets ? op.M / 128 + (E < op.M ? E : op.M) : E * ((op.M / E + 127) / 128);
+    a.tiles = (int)tiles;
+    return tiles * ((op.cols + 127) / 128) < 1 << 24;
+}
+
+hipError_t launch_quant_cols_grouped(const GroupedColOperand& op, const int32_t* offsets, int64_t E, int flags, hipStream_t st) {
+    if (op.M <= 0) return hipSuccess;
+    ColArgs a = col_args(op, offsets, E, flags);
+    if (!with_tiles(op, E, a)) return hipErrorInvalidValue;
+    cols_amax_kernel<<<xcd_grid((int64_t)a.tiles * ((op.cols + 511) / 512)), 256, 0, st>>>(a);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    return cast_cols(op, a, st);
+}
+
+hipError_t launch_quant_rows_cols_grouped(const GroupedColOperand& op, const int32_t* offsets, int64_t E, int flags, uint8_t* q, int64_t ld_q,
+                                          float* scale, hipStream_t st) {
+    if (op.M <= 0) return hipSuccess;
+    if (op.cols > 16384 || op.row_token || op.uniform) return hipErrorNotSupported;
+    // rows a tile: as many as one round of workgroups takes (four a CU, two with four pieces a thread), rounds of 64 rows at most
+    const int64_t cus = compute_units() > 0 ? compute_units() : 256, slots = cus * (op.cols <= 8192 ? 4 : 2), groups = E + 1 < op.M ? E + 1 : op.M;
+    const int64_t rounds = (op.M + 64 * slots - 1) / (64 * slots), room = rounds * slots - groups;
+    const int64_t height = room > 0 && (op.M + room - 1) / room > 16 ? (op.M + room - 1) / room : 16;
+    // (the maxima of the tiles, two bytes a column and tile, fit the codes' place)
+    if (2 * (op.M / height + groups) > op.ld_t) return hipErrorNotSupported;
+    ColArgs a = col_args(op, offsets, E, flags);
+    if (!with_tiles(op, E, a)) return hipErrorInvalidValue;
+    const unsigned grid = (unsigned)(op.M / height + groups);
+#define FP8K_BOTH(NV_)                                                                                                        \
+    do {                                                                                                                      \
+        if (op.fmt == FMT_E4M3FN) rows_cols_amax_kernel<FMT_E4M3FN, NV_><<<grid, 512, 0, st>>>(a, q, ld_q, scale, (int)height); \
+        else rows_cols_amax_kernel<FMT_E5M2, NV_><<<grid, 512, 0, st>>>(a, q, ld_q, scale, (int)height);                        \
+    } while (0)
+    if (op.cols <= 4096) FP8K_BOTH(1);
+    else if (op.cols <= 8192) FP8K_BOTH(2);
+    else FP8K_BOTH(4);
+#undef FP8K_BOTH
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    fold_tiles_kernel<<<dim3((unsigned)((op.cols + 511) / 512), (unsigned)E), 256, 0, st>>>(a, (int)height);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    return cast_cols(op, a, st);
 }
 
 }  // namespace fp8k

@@ -297,10 +297,17 @@ int fp8_grouped_linear_bwd(const void* dy, const void* x, int64_t T, const int32
         uint32_t *from = dx && !strips_w ? amax_w : amax_g, *to = dw && !strips_gx ? amax_x + E * K : amax_g;
         if (from < to) FP8_TRY(fp8k::launch_fill_u32(from, to - from, 0u, st));
     }
+    bool have_g = false;
     if (dx) {
         if (strips_w) FP8_TRY(fp8k::launch_quant_strips_grouped(cw, nullptr, offsets, E, fl, st));
         else FP8_TRY(fp8k::launch_quant_cols_grouped(cw, offsets, E, fl, st));
-        FP8_TRY(fp8k::launch_quant_rows_gather(dy, M, N, nullptr, M, N, recipe->fmt_dy, fl, ws + p.gq, ld, f32(p.sg), st));
+        // the gradient along both axes from two reads instead of three, where its columns are not read once by themselves
+        if (dw && !strips_gx) {
+            const hipError_t e = fp8k::launch_quant_rows_cols_grouped(cg, offsets, E, fl, ws + p.gq, ld, f32(p.sg), st);
+            have_g = e == hipSuccess;
+            if (!have_g && e != hipErrorNotSupported) FP8_TRY(e);
+        }
+        if (!have_g) FP8_TRY(fp8k::launch_quant_rows_gather(dy, M, N, nullptr, M, N, recipe->fmt_dy, fl, ws + p.gq, ld, f32(p.sg), st));
         FP8_TRY(fp8k::launch_gemm_fp8_grouped_rows({ws + p.gq, ld, recipe->fmt_dy, f32(p.sg), ws + p.wt, ld, recipe->fmt_w, f32(p.swt), offsets, E, M,
                                                     K, N, dx, K}, st));
     }
@@ -308,7 +315,7 @@ int fp8_grouped_linear_bwd(const void* dy, const void* x, int64_t T, const int32
         if (strips_gx) {
             FP8_TRY(fp8k::launch_quant_strips_grouped(cg, &cx, offsets, E, fl, st));
         } else {
-            FP8_TRY(fp8k::launch_quant_cols_grouped(cg, offsets, E, fl, st));
+            if (!have_g) FP8_TRY(fp8k::launch_quant_cols_grouped(cg, offsets, E, fl, st));
             FP8_TRY(fp8k::launch_quant_cols_grouped(cx, offsets, E, fl, st));
         }
         FP8_TRY(fp8k::launch_gemm_fp8_grouped_contract({ws + p.gt, Mp, recipe->fmt_dy, f32(p.sgt), ws + p.xt, Mp, recipe->fmt_x, f32(p.sxt), offsets,

@@ -39,6 +39,10 @@ struct GroupedColOperand {
     uint8_t* qt; int64_t ld_t; float* scale; uint32_t* amax;
 };
 hipError_t launch_quant_cols_grouped(const GroupedColOperand& op, const int32_t* offsets, int64_t E, int flags, hipStream_t st);
+// the same, and the rows' codes q and scales from the read that gathers the maxima (ragged groups of whole rows; hipErrorNotSupported, with
+// nothing launched: another operand, or longer rows)
+hipError_t launch_quant_rows_cols_grouped(const GroupedColOperand& op, const int32_t* offsets, int64_t E, int flags, uint8_t* q, int64_t ld_q,
+                                          float* scale, hipStream_t st);
 // the same for short groups, whose columns are read once: one operand or two (of groups of about the same length) in a launch
 hipError_t launch_quant_strips_grouped(const GroupedColOperand& op, const GroupedColOperand* second, const int32_t* offsets, int64_t E, int flags,
                                        hipStream_t st);

@@ -168,6 +168,9 @@ GROUPS = [
     ([0, 5, 0, 1, 0, 2] * 52, 200, 64, 112, 7),      # more groups than are looked up at a time
     ([3000, 1], 1500, 80, 160, 0),                   # a group that does not stay in registers
     ([20] * 40, 300, 96, 272, 0),
+    ([700, 0, 1500, 3], 400, 48, 4112, 5),           # long groups with long rows of the gradient: rows and maxima from one read
+    ([1, 1400], 100, 32, 8208, 0),
+    ([690], 64, 16, 16400, 2),                       # and rows too long for it
 ]
 RECIPES = {"row": {}, "pow2": {"flags": 1}, "swapped": {"fmt_x": 1, "fmt_w": 1, "fmt_dy": 0}}
 
