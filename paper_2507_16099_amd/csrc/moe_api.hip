@@ -132,6 +132,20 @@ int check_workspace(const char* fn, const void* ws, size_t have, size_t want) {
     return FP8_OK;
 }
 
+// zeros in launches that each count their threads in 32 bits
+hipError_t zero_words(void* to, int64_t words, hipStream_t st) {
+    constexpr int64_t most = (int64_t)1 << 31;
+    for (int64_t at = 0; at < words; at += most)
+        if (hipError_t e = fp8k::launch_fill_u32(static_cast<uint32_t*>(to) + at, words - at < most ? words - at : most, 0u, st); e != hipSuccess) return e;
+    return hipSuccess;
+}
+// an empty sum: K = 0 leaves Y = 0
+int zero_rows(const char* fn, void* y, int64_t M, int64_t N, hipStream_t st) {
+    FP8_CHECK(need(fn, "y", y, 16));
+    FP8_TRY(zero_words(y, M * N / 2, st));
+    return FP8_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -243,7 +257,8 @@ int fp8_grouped_linear_fwd(const void* x, int64_t T, const int32_t* row_token, c
     FP8_CHECK(check_recipe(fn, recipe));
     FP8_CHECK(check_dims(fn, T, M, E, K, N, false));
     FP8_CHECK(check_rows(fn, row_token, T, M));
-    if (M == 0 || N == 0 || K == 0) return FP8_OK;
+    if (M == 0 || N == 0) return FP8_OK;
+    if (K == 0) return zero_rows(fn, y, M, N, static_cast<hipStream_t>(stream));
     FP8_CHECK(need(fn, "offsets", offsets, 4));
     FP8_CHECK(need(fn, "y", y, 16));
     FP8_CHECK(need(fn, "w", w, 16));
@@ -269,11 +284,12 @@ int fp8_grouped_linear_bwd(const void* dy, const void* x, int64_t T, const int32
     FP8_CHECK(check_recipe(fn, recipe));
     FP8_CHECK(check_dims(fn, T, M, E, K, N, true));
     FP8_CHECK(check_rows(fn, row_token, T, M));
-    if (K == 0 || N == 0 || (!dx && !dw)) return FP8_OK;
+    if (K == 0 || (!dx && !dw)) return FP8_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (!aligned(dx, 16) || !aligned(dw, 16)) return fail(FP8_ERR_ALIGN, "%s: dx, dw not 16-byte aligned", fn);
-    if (M == 0) {      // no rows: the weights' gradients are zero
-        if (dw) FP8_TRY(fp8k::launch_fill_u32(static_cast<uint32_t*>(dw), E * N * K / 2, 0u, st));
+    if (M == 0 || N == 0) {      // empty sums
+        if (dx) FP8_TRY(zero_words(dx, M * K / 2, st));
+        if (dw) FP8_TRY(zero_words(dw, E * N * K / 2, st));
         return FP8_OK;
     }
     FP8_CHECK(need(fn, "offsets", offsets, 4));
@@ -295,7 +311,7 @@ int fp8_grouped_linear_bwd(const void* dy, const void* x, int64_t T, const int32
     const bool strips_w = fp8k::grouped_strips(cw, E), strips_gx = fp8k::grouped_strips(cg, E);
     {
         uint32_t *from = dx && !strips_w ? amax_w : amax_g, *to = dw && !strips_gx ? amax_x + E * K : amax_g;
-        if (from < to) FP8_TRY(fp8k::launch_fill_u32(from, to - from, 0u, st));
+        FP8_TRY(zero_words(from, to - from, st));
     }
     bool have_g = false;
     if (dx) {
@@ -343,7 +359,8 @@ int fp8_grouped_linear_fwd_prequantized(const void* x, int64_t T, const int32_t*
     FP8_CHECK(check_rows(fn, row_token, T, M));
     FP8_CHECK(need_ld(fn, "wq", ldw, K, 16));
     if (ldw > kMaxLd) return fail(FP8_ERR_SHAPE, "%s: ldw=%lld out of range", fn, (ll)ldw);
-    if (M == 0 || N == 0 || K == 0) return FP8_OK;
+    if (M == 0 || N == 0) return FP8_OK;
+    if (K == 0) return zero_rows(fn, y, M, N, static_cast<hipStream_t>(stream));
     FP8_CHECK(need(fn, "offsets", offsets, 4));
     FP8_CHECK(need(fn, "y", y, 16));
     FP8_CHECK(need(fn, "scale_w", scale_w, 4));

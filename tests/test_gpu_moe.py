@@ -388,3 +388,20 @@ def test_layer_replays_from_a_graph():
         torch.cuda.synchronize()
         for a, b in zip(got, outs):
             assert torch.equal(a, b), n
+
+
+def test_empty_sums_are_zero():
+    offsets, row_token = torch.tensor([0, 2, 5], dtype=torch.int32).cuda(), torch.zeros(5, dtype=torch.int32).cuda()
+    r = fp8.Recipe(gran=fp8.FP8_ROW)
+    bf16 = dict(dtype=BF16, device="cuda")
+    y = torch.full((5, 24), 7.0, **bf16)
+    fp8.fp8_grouped_linear_fwd(torch.empty((1, 0), **bf16), torch.empty((2, 24, 0), **bf16), offsets, r, row_token=row_token, y=y)
+    assert (y == 0).all()
+    dx = torch.full((5, 48), 7.0, **bf16)
+    fp8.fp8_grouped_linear_bwd(torch.empty((5, 0), **bf16), torch.randn((1, 48), **bf16), torch.empty((2, 0, 48), **bf16), offsets, r,
+                               row_token=row_token, dx=dx, need_dw=False)
+    assert (dx == 0).all()
+    # no rows at all: zeros for the weights
+    none, dw = fp8.fp8_grouped_linear_bwd(torch.empty((0, 32), **bf16), torch.empty((0, 48), **bf16), torch.randn((2, 32, 48), **bf16),
+                                          torch.zeros(3, dtype=torch.int32, device="cuda"), r, dw=torch.full((2, 32, 48), 7.0, **bf16), need_dx=False)
+    assert (dw == 0).all()
