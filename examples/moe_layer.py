@@ -1,0 +1,146 @@
+"""A mixture-of-experts layer trained and served in float8: router, experts, combination, their gradients and the AdamW step.
+
+    python examples/moe_layer.py                      # 8192 tokens, 8 experts of 2048 -> 5632 -> 2048, 2 per token
+    python examples/moe_layer.py --tokens 1024 --dim 512 --hidden 1024 --experts 32 --k 4 --steps 50
+
+    gates, experts, row lists = choice(x Wr^T)                       fp8_moe_route
+    h[r] = x[token of r] W1[e]^T;  a = silu(h);  y = a W2[e]^T       fp8_grouped_linear_fwd
+    out[t] = sum_j gate[t, j] y[row of t, j]                         fp8_moe_combine
+
+The gradients are written out call by call, without a tape: every buffer has its place, so the whole step runs on one stream with
+no host synchronisation.  The experts' products hold nearly all of the work; silu and the router's small projection are plain torch.
+"""
+import argparse
+import os
+import sys
+
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+import paper_2507_16099_amd as fp8  # noqa: E402
+
+ROW = fp8.Recipe(gran=fp8.FP8_ROW)      # e4m3 activations and weights, e5m2 gradients, one scale per row of each contraction
+
+
+class MoeLayer:
+    def __init__(self, dim, hidden, experts, k, device="cuda", seed=0):
+        g = torch.Generator(device=device).manual_seed(seed)
+
+        def weight(*shape):
+            return (torch.randn(shape, generator=g, device=device) * shape[-1] ** -0.5).to(torch.bfloat16)
+
+        self.k, self.flags = k, fp8.FP8_ROUTE_RENORM
+        self.wr, self.w1, self.w2 = weight(experts, dim), weight(experts, hidden, dim), weight(experts, dim, hidden)
+        self.params = [self.wr, self.w1, self.w2]
+        self.grads = [torch.zeros_like(p) for p in self.params]
+        self.steps = 0
+
+    def forward(self, x):
+        """x [T, dim] -> [T, dim]; keeps what the backward needs."""
+        logits = x.float() @ self.wr.float().T
+        route = fp8.fp8_moe_route(logits, self.k, self.flags)
+        gates, _, offsets, row_token, slot_row = route
+        h = fp8.fp8_grouped_linear_fwd(x, self.w1, offsets, ROW, row_token=row_token)
+        a = torch.nn.functional.silu(h)
+        y = fp8.fp8_grouped_linear_fwd(a, self.w2, offsets, ROW)
+        self.kept = x, logits, route, h, a, y
+        return fp8.fp8_moe_combine(y, gates, slot_row)
+
+    def backward(self, dout):
+        """The gradient of the last forward's x; those of the parameters go to self.grads."""
+        x, logits, (gates, experts, offsets, row_token, slot_row), h, a, y = self.kept
+        dwr, dw1, dw2 = self.grads
+        dy, dgates = fp8.fp8_moe_combine_bwd(dout, y, gates, slot_row, row_token)
+        da, _ = fp8.fp8_grouped_linear_bwd(dy, a, self.w2, offsets, ROW, dw=dw2)
+        s = torch.sigmoid(h.float())
+        dh = (da.float() * s * (1 + h.float() * (1 - s))).to(torch.bfloat16)
+        dx_rows, _ = fp8.fp8_grouped_linear_bwd(dh, x, self.w1, offsets, ROW, row_token=row_token, dw=dw1)
+        dlogits = fp8.fp8_moe_route_bwd(dgates, logits, gates, experts, self.flags)
+        dwr.copy_(dlogits.T @ x.float())
+        dx = fp8.fp8_moe_combine(dx_rows, None, slot_row)      # the rows of a token, summed
+        return (dx.float() + dlogits @ self.wr.float()).to(torch.bfloat16)
+
+    def optimizer(self):
+        """Moments in 8 bits, and the table by which one launch finds all tensors."""
+        def codes(p):
+            return torch.zeros(p.numel(), dtype=torch.uint8, device=p.device)
+
+        def scales(p):
+            return torch.ones(-(-p.numel() // fp8.FP8_ADAMW_BLOCK), device=p.device)
+
+        ps = self.params
+        self.adamw = fp8.fp8_adamw_tensors(ps, self.grads, [codes(p) for p in ps], [codes(p) for p in ps], [scales(p) for p in ps],
+                                           [scales(p) for p in ps])
+
+    def step(self, lr, weight_decay=0.0):
+        self.steps += 1
+        fp8.fp8_adamw_step(self.adamw, lr, self.steps, weight_decay=weight_decay)
+
+    def freeze(self):
+        """The experts' weights quantized once, for serving."""
+        def quantize(w):
+            E, N, K = w.shape
+            q, s = fp8.fp8_quantize(w.view(E * N, K), fp8.FP8_ROW, ROW.fmt_w)
+            return q.view(E, N, K), s.view(E, N)
+
+        self.q1, self.q2 = quantize(self.w1), quantize(self.w2)
+
+    def serve(self, x):
+        """forward against the frozen weights, nothing kept."""
+        gates, _, offsets, row_token, slot_row = fp8.fp8_moe_route(x.float() @ self.wr.float().T, self.k, self.flags)
+        h = fp8.fp8_grouped_linear_fwd_prequantized(x, self.q1[0], ROW.fmt_w, self.q1[1], offsets, row_token=row_token)
+        y = fp8.fp8_grouped_linear_fwd_prequantized(torch.nn.functional.silu(h), self.q2[0], ROW.fmt_w, self.q2[1], offsets)
+        return fp8.fp8_moe_combine(y, gates, slot_row)
+
+
+def train(layer, x, target, steps, lr):
+    """Mean squared error against target, full batches; returns the losses."""
+    layer.optimizer()
+    losses = []
+    for _ in range(steps):
+        err = layer.forward(x).float() - target
+        losses.append((err * err).mean())
+        layer.backward((err * (2.0 / err.numel())).to(torch.bfloat16))
+        layer.step(lr)
+    return torch.stack(losses).tolist()
+
+
+def main():
+    ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
+    for name, value in (("tokens", 8192), ("dim", 2048), ("hidden", 5632), ("experts", 8), ("k", 2), ("steps", 20), ("decode", 4)):
+        ap.add_argument(f"--{name}", type=int, default=value)
+    ap.add_argument("--lr", type=float, default=1e-3)
+    args = ap.parse_args()
+    g = torch.Generator(device="cuda").manual_seed(1)
+    layer = MoeLayer(args.dim, args.hidden, args.experts, args.k)
+    x = torch.randn((args.tokens, args.dim), generator=g, device="cuda").to(torch.bfloat16)
+    target = torch.tanh(x.float().roll(1, 1))
+
+    def timed(fn, n):
+        fn()
+        start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        start.record()
+        for _ in range(n):
+            fn()
+        end.record()
+        end.synchronize()
+        return start.elapsed_time(end) / n
+
+    losses = train(layer, x, target, args.steps, args.lr)
+    print(f"loss {losses[0]:.4f} -> {losses[-1]:.4f} in {args.steps} steps", flush=True)
+    dout = torch.randn_like(x)
+
+    def whole():
+        layer.forward(x)
+        layer.backward(dout)
+        layer.step(0.0)
+
+    print(f"training step of {args.tokens} tokens: {timed(whole, 10):.3f} ms", flush=True)
+    layer.freeze()
+    some = x[:args.decode]
+    same = (layer.serve(some).float() - layer.forward(some).float()).norm() / layer.forward(some).float().norm()
+    print(f"served with weights quantized once: {args.decode} tokens {timed(lambda: layer.serve(some), 50) * 1e3:.0f} us, off by {same.item():.1e}", flush=True)
+
+
+if __name__ == "__main__":
+    main()
