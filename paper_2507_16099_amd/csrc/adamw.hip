@@ -12,8 +12,10 @@
 //
 // One launch, however many tensors: the caller keeps a table in device memory that has each workgroup's piece of a tensor ready, so that one load
 // leads to the data (a search through the sizes, or a list of pieces that names tensors, is a chain of them).  Pieces are 2048
-// elements, one trip of a workgroup, or where that makes more workgroups than PLENTY, 8192.
-// Bound: HBM, 10 bytes an element (bfloat16, 8-bit moments) to 28 (all binary32).
+// elements, eight a thread; four such trips a workgroup, with a quarter of the table, are slower: 67 million elements 134 us
+// against 125 with 8-bit moments, 297 against 267 with 32-bit ones.
+// Bound: HBM, 10 bytes an element (bfloat16, 8-bit moments) to 28 (all binary32).  Measured: eight tensors of 58.7 million elements
+// 805 us (5.4 TB/s); 150 of 8192, all binary32, 9 us.
 #include "fp8_device.hpp"
 #include "moe_launchers.hpp"
 
@@ -24,8 +26,7 @@ namespace fp8k {
 namespace {
 
 constexpr int NT = 256;
-constexpr int TRIP = NT * 8;          // elements of a workgroup at a time
-constexpr int64_t PLENTY = 16384;     // workgroups
+constexpr int PIECE = NT * 8;         // elements of a workgroup
 
 struct Update {
     AdamwScalars s;
@@ -134,63 +135,61 @@ __device__ __forceinline__ float state_scale(float amax) {
 // 1 / s of a power of two; of zero (a state that was never written) something finite
 __device__ __forceinline__ float inverse_pow2(float s) { return __uint_as_float((254u - (__float_as_uint(s) >> 23 & 0xFFu)) << 23); }
 
-// a thread: eight elements at a time; 32 lanes hold a block of 256
+// a thread: eight elements; 32 lanes hold a block of 256
 template <class P, class G, bool FP8>
 __global__ __launch_bounds__(NT) void adamw_kernel(const AdamwHeader* __restrict__ table, int flags, AdamwScalars s) {
     // (requested together; a table made for other types, or for fewer workgroups, changes nothing)
     const AdamwPiece t = reinterpret_cast<const AdamwPiece*>(table + 1)[blockIdx.x];
     const int64_t blocks = table->blocks;
-    const int made_for = table->flags, rounds = table->rounds;
+    const int made_for = table->flags;
     if (made_for != flags || (int64_t)blockIdx.x >= blocks) return;
     const Update u{s, s.grad_scale ? *s.grad_scale : 1.0f};
     P* p = static_cast<P*>(t.p);
     const G* g = static_cast<const G*>(t.g);
-    for (int r = 0; r < rounds; ++r) {
-        const int64_t i = (int64_t)(r * NT + (int)threadIdx.x) * 8;
-        const int64_t left = t.n - i;
-        const int n = left >= 8 ? 8 : left > 0 ? (int)left : 0;
-        if (!FP8 && n == 0) return;
-        float fp[8], fg[8], m[8], v[8], root[8];
-        load8(p + i, n, fp);
-        load8(g + i, n, fg);
-        if constexpr (FP8) {
-            const float inv_m = n ? inverse_pow2(t.sm[i / 256]) : 0.f, inv_v = n ? inverse_pow2(t.sv[i / 256]) : 0.f;
-            load_codes(static_cast<const uint8_t*>(t.m) + i, n, m);
-            load_codes(static_cast<const uint8_t*>(t.v) + i, n, root);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                m[e] *= inv_m;
-                const float ro = root[e] * inv_v;
-                v[e] = ro * ro;      // (eight significant bits: exact)
-            }
-        } else {
-            load8(static_cast<const float*>(t.m) + i, n, m);
-            load8(static_cast<const float*>(t.v) + i, n, v);
-        }
+    const int i = (int)threadIdx.x * 8;
+    const int64_t left = t.n - i;
+    const int n = left >= 8 ? 8 : left > 0 ? (int)left : 0;
+    if (!FP8 && n == 0) return;
+    float fp[8], fg[8], m[8], v[8], root[8];
+    load8(p + i, n, fp);
+    load8(g + i, n, fg);
+    if constexpr (FP8) {
+        const float inv_m = n ? inverse_pow2(t.sm[i / 256]) : 0.f, inv_v = n ? inverse_pow2(t.sv[i / 256]) : 0.f;
+        load_codes(static_cast<const uint8_t*>(t.m) + i, n, m);
+        load_codes(static_cast<const uint8_t*>(t.v) + i, n, root);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            u.moments(fg[e], m[e], v[e]);
-            root[e] = __fsqrt_rn(v[e]);
-            fp[e] = u.param(fp[e], m[e], root[e]);
+            m[e] *= inv_m;
+            const float ro = root[e] * inv_v;
+            v[e] = ro * ro;      // (eight significant bits: exact)
         }
-        store8(p + i, n, fp);
-        if constexpr (FP8) {
-            const float sm = state_scale(block_amax(m)), sv = state_scale(block_amax(root));
+    } else {
+        load8(static_cast<const float*>(t.m) + i, n, m);
+        load8(static_cast<const float*>(t.v) + i, n, v);
+    }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                m[e] *= sm;
-                root[e] = root[e] > 0.f ? fmaxf(root[e] * sv, 0x1p-9f) : root[e];
-            }
-            store_codes(static_cast<uint8_t*>(t.m) + i, n, m);
-            store_codes(static_cast<uint8_t*>(t.v) + i, n, root);
-            if (n && threadIdx.x % 32 == 0) {
-                t.sm[i / 256] = sm;
-                t.sv[i / 256] = sv;
-            }
-        } else {
-            store8(static_cast<float*>(t.m) + i, n, m);
-            store8(static_cast<float*>(t.v) + i, n, v);
+    for (int e = 0; e < 8; ++e) {
+        u.moments(fg[e], m[e], v[e]);
+        root[e] = __fsqrt_rn(v[e]);
+        fp[e] = u.param(fp[e], m[e], root[e]);
+    }
+    store8(p + i, n, fp);
+    if constexpr (FP8) {
+        const float sm = state_scale(block_amax(m)), sv = state_scale(block_amax(root));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            m[e] *= sm;
+            root[e] = root[e] > 0.f ? fmaxf(root[e] * sv, 0x1p-9f) : root[e];
         }
+        store_codes(static_cast<uint8_t*>(t.m) + i, n, m);
+        store_codes(static_cast<uint8_t*>(t.v) + i, n, root);
+        if (n && threadIdx.x % 32 == 0) {
+            t.sm[i / 256] = sm;
+            t.sv[i / 256] = sv;
+        }
+    } else {
+        store8(static_cast<float*>(t.m) + i, n, m);
+        store8(static_cast<float*>(t.v) + i, n, v);
     }
 }
 
@@ -202,18 +201,11 @@ hipError_t launch_t(const void* table, int64_t blocks, int flags, const AdamwSca
     return hipGetLastError();
 }
 
-int64_t pieces(int64_t n, int rounds) { return (n + (int64_t)rounds * TRIP - 1) / ((int64_t)rounds * TRIP); }
-
 }  // namespace
 
 AdamwHeader adamw_header(const AdamwTensor* tensors, int64_t count, int flags) {
-    AdamwHeader h{0, flags, 1, {}};
-    for (int64_t i = 0; i < count; ++i) h.blocks += pieces(tensors[i].n, 1);
-    if (h.blocks > PLENTY) {
-        h.rounds = 4;
-        h.blocks = 0;
-        for (int64_t i = 0; i < count; ++i) h.blocks += pieces(tensors[i].n, 4);
-    }
+    AdamwHeader h{0, flags, 0, {}};
+    for (int64_t i = 0; i < count; ++i) h.blocks += (tensors[i].n + PIECE - 1) / PIECE;
     if (h.blocks > (1 << 24) - 1) h.blocks = -1;      // (a grid's threads are counted in 32 bits)
     return h;
 }
@@ -223,13 +215,12 @@ void adamw_fill_table(const AdamwTensor* tensors, int64_t count, const AdamwHead
     std::memcpy(at, &h, sizeof(h));
     at += sizeof(h);
     const bool p_f32 = h.flags & ADAMW_PARAM_FP32, g_f32 = h.flags & ADAMW_GRAD_FP32, q = h.flags & ADAMW_STATE_FP8;
-    const int64_t size = (int64_t)h.rounds * TRIP;
     for (int64_t i = 0; i < count; ++i) {
         const AdamwTensor& t = tensors[i];
-        for (int64_t d = 0; d < t.n; d += size, at += sizeof(AdamwPiece)) {
+        for (int64_t d = 0; d < t.n; d += PIECE, at += sizeof(AdamwPiece)) {
             const AdamwPiece piece{static_cast<char*>(t.p) + d * (p_f32 ? 4 : 2), static_cast<const char*>(t.g) + d * (g_f32 ? 4 : 2),
                                    static_cast<char*>(t.m) + d * (q ? 1 : 4), static_cast<char*>(t.v) + d * (q ? 1 : 4),
-                                   q ? t.sm + d / 256 : nullptr, q ? t.sv + d / 256 : nullptr, t.n - d < size ? t.n - d : size, 0};
+                                   q ? t.sm + d / 256 : nullptr, q ? t.sv + d / 256 : nullptr, t.n - d < PIECE ? t.n - d : PIECE, 0};
             std::memcpy(at, &piece, sizeof(piece));
         }
     }

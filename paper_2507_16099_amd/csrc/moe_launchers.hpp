@@ -46,8 +46,16 @@ hipError_t launch_quant_rows_cols_grouped(const GroupedColOperand& op, const int
 // the same for short groups, whose columns are read once: one operand or two (of groups of about the same length) in a launch
 hipError_t launch_quant_strips_grouped(const GroupedColOperand& op, const GroupedColOperand* second, const int32_t* offsets, int64_t E, int flags,
                                        hipStream_t st);
-// whether that form is taken
-inline bool grouped_strips(const GroupedColOperand& op, int64_t E) { return op.M / E <= (op.uniform ? 2560 : 640); }
+// Whether that form is taken: up to as many rows a group as stay in registers without many spans (us, maxima and cast / strips): weights'
+// columns in dX, eight experts, 2560 x 2048 62 / 54, 4096 x 2048 90 / 98, 14336 x 4096 598 / 706; gradient and activations in dW, eight
+// ragged groups of 640 rows on average (4096 x 4096) 135 / 129, of 1000 (4096 x 2048) 116 / 108, of 1024 (14336 x 2048) 402 / 391, of 1500
+// (1408 x 2048) 80 / 85.
+inline bool grouped_strips(const GroupedColOperand& op, int64_t E) { return op.M / E <= (op.uniform ? 2560 : 1024); }
+// Whether the gradient's rows and its columns' maxima come from one read, where both are wanted: where it is too large for the last-level
+// cache to keep for a third one (whole backward in us, three reads / this): 16384 x 8192 807 / 785, 16384 x 14336 874 / 799, and
+// against strips for 8192 x 14336 in groups of 1024, 925 / 904; below, 16384 x 5632 844 / 864, 12000 x 1408 150 / 157.  Not where groups
+// are short: strips read it once.
+inline bool grouped_rows_cols(int64_t M, int64_t N, int64_t E) { return M * N >= (int64_t)96 << 20 && M / E > 640; }
 // columns that the padded groups of M rows can come to
 inline int64_t grouped_padded(int64_t M, int64_t E) { return (M + 127 * (E < M ? E : M) + 127) / 128 * 128; }
 
@@ -76,7 +84,7 @@ struct AdamwTensor { void* p; const void* g; void *m, *v; float *sm, *sv; int64_
 constexpr int ADAMW_PARAM_FP32 = 256, ADAMW_GRAD_FP32 = 512, ADAMW_STATE_FP8 = 1024;      // of the ABI's flags
 struct AdamwScalars { float b1, c1, b2, c2, decay, rate, inv_root, eps; const float* grad_scale; };
 // The table in device memory that a step reads: a header, and for each workgroup its piece of a tensor, all pointers moved to it.
-struct AdamwHeader { int64_t blocks; int32_t flags, rounds; int64_t reserved[6]; };
+struct AdamwHeader { int64_t blocks; int32_t flags, zero; int64_t reserved[6]; };
 struct AdamwPiece { void* p; const void* g; void *m, *v; float *sm, *sv; int64_t n, reserved; };
 static_assert(sizeof(AdamwHeader) == 64 && sizeof(AdamwPiece) == 64, "whole pieces of a cache line");
 AdamwHeader adamw_header(const AdamwTensor* tensors, int64_t count, int flags);      // blocks < 0: too many

@@ -154,23 +154,21 @@ def test_adamw_table(lib, p):
 
 @pytest.mark.parametrize("sizes", [[1], [2048, 2049, 0, 5], [16384 * 2048, 1], [16384 * 2048 + 1, 8193, 0, 3]])
 def test_adamw_table_covers_every_element_once(sizes):
-    """A header (blocks, flags, rounds), then 64 bytes for each workgroup: the pointers of its piece and how long it is."""
+    """A header (blocks, flags), then 64 bytes for each workgroup: the pointers of its piece and how long it is."""
     import numpy as np
     base = [1 << 44, 2 << 44, 3 << 44, 4 << 44, 5 << 44, 6 << 44]
     for flags, bytes_of in ((0, (2, 2, 4, 4)), (fp8.FP8_ADAMW_PARAM_FP32 | fp8.FP8_ADAMW_STATE_FP8, (4, 2, 1, 1)), (fp8.FP8_ADAMW_GRAD_FP32, (2, 4, 4, 4))):
         array = (_CAdamwTensor * len(sizes))(*[_CAdamwTensor(*[b + (i << 40) for b in base], n) for i, n in enumerate(sizes)])
         table, blocks = fp8.fp8_adamw_table(array, len(sizes), flags)
         raw = table.numpy()
-        rounds = raw[12:16].view(np.int32)[0]
         assert raw[:8].view(np.int64)[0] == blocks and raw[8:12].view(np.int32)[0] == flags
-        assert rounds == (1 if sum(-(-n // 2048) for n in sizes) <= 16384 else 4)
         pieces = raw[64:].view(np.int64).reshape(-1, 8)
         assert len(pieces) == blocks
         want, q = [], flags & fp8.FP8_ADAMW_STATE_FP8
         for i, n in enumerate(sizes):
-            for d in range(0, n, 2048 * rounds):
+            for d in range(0, n, 2048):
                 ptrs = [b + (i << 40) + d * s for b, s in zip(base, bytes_of)] + [b + (i << 40) + d // 256 * 4 if q else 0 for b in base[4:]]
-                want.append(ptrs + [min(n - d, 2048 * rounds), 0])
+                want.append(ptrs + [min(n - d, 2048), 0])
         assert np.array_equal(pieces, np.array(want, dtype=np.int64).reshape(-1, 8))
 
 
