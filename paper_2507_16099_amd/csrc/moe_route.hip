@@ -14,8 +14,8 @@
 // bit of the expert's number, so ranks, and the lists, come out in order and alike every time, without atomics on positions.
 // A few tokens (one chunk) take one launch.
 //
-// Bound: 16 tokens of 64 experts are a launch's latency; 16384 tokens of 64 experts read 4 MB and write 1.6 MB, far less than what
-// the rounds and the two launches take.
+// Bound: 16 tokens of 64 experts are a launch's latency and the chain of its rounds, 5.8 us; 16384 tokens of 64 experts read 4 MB and write
+// 1.6 MB, far less than what the rounds and the two launches take: choice 5.6 us, lists 6.4, gradient 5.8.
 #include "moe_launchers.hpp"
 
 namespace fp8k {
@@ -329,10 +329,12 @@ int64_t chunk_of(int64_t T) { return (T + MAX_CHUNKS - 1) / MAX_CHUNKS; }
 
 }  // namespace
 
-// tokens that one workgroup takes by itself
-static bool one_chunk(int64_t T) { return T <= 64; }
+// Tokens that one workgroup takes by itself: as many as it has groups of lanes, or twice that of up to 64 experts (us, in one launch / two):
+// 64 experts, 64, 128, 160 tokens 5.9 8.5 11.1 / 9.8 9.6 10.0; 128 experts, 64, 128 tokens 8.4 13.3 / 11.9 12.6; 256 experts, 32, 64
+// tokens 9.4 14.7 / 12.8 13.5; 512 experts, sixteen choices, 16, 32 tokens 15.2 24.5 / 18.7 19.2.
+static bool one_chunk(int64_t T, int64_t E) { return T <= (E <= 64 ? 128 : E <= 128 ? 64 : E <= 256 ? 32 : 16); }
 
-size_t route_workspace_bytes(int64_t T, int64_t E) { return one_chunk(T) ? 256 : (size_t)MAX_CHUNKS * (size_t)E * 4; }
+size_t route_workspace_bytes(int64_t T, int64_t E) { return one_chunk(T, E) ? 256 : (size_t)MAX_CHUNKS * (size_t)E * 4; }
 
 #define FP8K_ROUTE_FORMS(E_, CALL)          \
     if (E_ <= 16) { CALL(16, 1); }          \
@@ -346,7 +348,7 @@ hipError_t launch_moe_route(const void* logits, bool f32, int64_t T, int64_t E, 
                             int32_t* offsets, int32_t* row_token, int32_t* slot_row, void* ws, hipStream_t st) {
     RouteArgs a{logits, f32, (int)T, (int)E, k, renorm, 0, ld, gates, experts, offsets, row_token, slot_row, static_cast<int32_t*>(ws)};
     const int lds = (int)(20 * E + 1) * 4;
-    if (one_chunk(T)) {
+    if (one_chunk(T, E)) {
         a.chunk = (int)T;
 #define FP8K_CALL(L_, V_) route_choose_kernel<L_, V_, true><<<1, NT, lds, st>>>(a)
         FP8K_ROUTE_FORMS(E, FP8K_CALL)
