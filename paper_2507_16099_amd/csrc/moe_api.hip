@@ -3,6 +3,7 @@
 #include "../../include/fp8mi355.h"
 #include "launchers.hpp"
 #include "moe_launchers.hpp"
+#include "tuning.hpp"
 
 #include <cmath>
 #include <cstdarg>
@@ -56,7 +57,7 @@ int need_ld(const char* fn, const char* what, int64_t ld, int64_t cols, int64_t 
 
 int check_route(const char* fn, int64_t T, int64_t E, int64_t ld, int k, int flags) {
     if (flags & ~(FP8_ROUTE_RENORM | FP8_ROUTE_FP32)) return fail(FP8_ERR_ENUM, "%s: flags=%d has unknown bits", fn, flags);
-    if (T < 0 || T > kMaxDim) return fail(FP8_ERR_SHAPE, "%s: T=%lld out of range", fn, (ll)T);
+    if (T < 0 || T > (int64_t)1 << 30) return fail(FP8_ERR_SHAPE, "%s: T=%lld out of range", fn, (ll)T);      // (kernels count ahead of the last)
     if (E < 1 || E > fp8k::ROUTE_MAX_EXPERTS) return fail(FP8_ERR_SHAPE, "%s: E=%lld, 1 .. %d are supported", fn, (ll)E, fp8k::ROUTE_MAX_EXPERTS);
     if (k < 1 || k > fp8k::ROUTE_MAX_K || k > E) return fail(FP8_ERR_SHAPE, "%s: k=%d, 1 .. min(E, %d) are supported", fn, k, fp8k::ROUTE_MAX_K);
     if (T * k > kMaxDim) return fail(FP8_ERR_SHAPE, "%s: T k = %lld out of range", fn, (ll)(T * k));
@@ -308,7 +309,10 @@ int fp8_grouped_linear_bwd(const void* dy, const void* x, int64_t T, const int32
     const fp8k::GroupedColOperand cw{w, E * N, K, nullptr, E * N, K, recipe->fmt_w, true, ws + p.wt, ld, f32(p.swt), amax_w};
     const fp8k::GroupedColOperand cg{dy, M, N, nullptr, M, N, recipe->fmt_dy, false, ws + p.gt, Mp, f32(p.sgt), amax_g};
     const fp8k::GroupedColOperand cx{x, T, K, row_token, M, K, recipe->fmt_x, false, ws + p.xt, Mp, f32(p.sxt), amax_x};
-    const bool strips_w = fp8k::grouped_strips(cw, E), strips_gx = fp8k::grouped_strips(cg, E);
+    const int strips = fp8k::knob(fp8k::KNOB_STRIPS);      // 0: never, and rows and maxima from one read wherever that fits; 2, 4: always
+    const bool rows_cols = dx && dw && (strips == 0 || (strips < 0 && fp8k::grouped_rows_cols(M, N, E)));
+    const bool strips_w = strips != 0 && (strips > 0 || fp8k::grouped_strips(cw, E));
+    const bool strips_gx = !rows_cols && strips != 0 && (strips > 0 || fp8k::grouped_strips(cg, E));
     {
         uint32_t *from = dx && !strips_w ? amax_w : amax_g, *to = dw && !strips_gx ? amax_x + E * K : amax_g;
         FP8_TRY(zero_words(from, to - from, st));
@@ -317,8 +321,7 @@ int fp8_grouped_linear_bwd(const void* dy, const void* x, int64_t T, const int32
     if (dx) {
         if (strips_w) FP8_TRY(fp8k::launch_quant_strips_grouped(cw, nullptr, offsets, E, fl, st));
         else FP8_TRY(fp8k::launch_quant_cols_grouped(cw, offsets, E, fl, st));
-        // the gradient along both axes from two reads instead of three, where its columns are not read once by themselves
-        if (dw && !strips_gx) {
+        if (rows_cols) {
             const hipError_t e = fp8k::launch_quant_rows_cols_grouped(cg, offsets, E, fl, ws + p.gq, ld, f32(p.sg), st);
             have_g = e == hipSuccess;
             if (!have_g && e != hipErrorNotSupported) FP8_TRY(e);

@@ -1,6 +1,6 @@
 // Sanitizer driver for the HOST side of the mixture-of-experts and AdamW entry points (test infrastructure).
 //
-// Built by tests/test_moe_sanitizers.py from this file, moe_api.hip and adamw.hip (for its table) with AddressSanitizer and
+// Built by tests/test_moe_sanitizers.py from this file, moe_api.hip, tuning.hip and adamw.hip (for its table) with AddressSanitizer and
 // UndefinedBehaviorSanitizer on the host code only.  The other kernels' launchers are the stubs below: they touch nothing but check that
 // every place handed to them lies inside the workspace that was asked for and overlaps no other of the same call.
 #include "../include/fp8mi355.h"

@@ -168,9 +168,9 @@ GROUPS = [
     ([0, 5, 0, 1, 0, 2] * 52, 200, 64, 112, 7),      # more groups than are looked up at a time
     ([3000, 1], 1500, 80, 160, 0),                   # a group that does not stay in registers
     ([20] * 40, 300, 96, 272, 0),
-    ([700, 0, 1500, 3], 400, 48, 4112, 5),           # long groups with long rows of the gradient: rows and maxima from one read
+    ([700, 0, 1500, 3], 400, 48, 4112, 5),           # long groups with long rows of the gradient
     ([1, 1400], 100, 32, 8208, 0),
-    ([690], 64, 16, 16400, 2),                       # and rows too long for it
+    ([690], 64, 16, 16400, 2),
 ]
 RECIPES = {"row": {}, "pow2": {"flags": 1}, "swapped": {"fmt_x": 1, "fmt_w": 1, "fmt_dy": 0}}
 
@@ -262,6 +262,20 @@ def test_every_form_of_the_products(case):
             ref.assert_product(y.cpu(), want, size)
             ref.assert_product(dx.cpu(), want_dx, size_dx)
             ref.assert_product(dw.cpu(), want_dw, size_dw)
+
+
+@pytest.mark.parametrize("case", range(len(GROUPS)))
+def test_every_way_to_the_operands_gives_the_same_codes(case):
+    """Strips, maxima and cast, rows and maxima from one read: the operands of a product are the same, so is what comes out."""
+    sizes, T, K, N, tail = GROUPS[case]
+    offsets, row_token, x, w, dy = _case(sizes, T, K, N, 500 + case, tail)
+    for r in (fp8.Recipe(gran=fp8.FP8_ROW), fp8.Recipe(gran=fp8.FP8_ROW, fmt_x=1, fmt_w=1, fmt_dy=0, flags=1)):
+        outs = []
+        for strips in (-1, 0, 2):
+            with knobs(STRIPS=strips):
+                outs.append(fp8.fp8_grouped_linear_bwd(dy.cuda(), x.cuda(), w.cuda(), offsets.cuda(), r, row_token=row_token.cuda()))
+        for dx, dw in outs[1:]:
+            assert torch.equal(dx.view(torch.int16), outs[0][0].view(torch.int16)) and torch.equal(dw.view(torch.int16), outs[0][1].view(torch.int16))
 
 
 @pytest.mark.parametrize("offsets", [[0, 50, 20, 90, 200, -5], [0, -3, -4, 1 << 30, 7, 100], [7, 7, 7, 7, 7, 7], [0, 2147483647, -2147483648, 60, 40, 100]])

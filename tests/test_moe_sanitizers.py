@@ -15,7 +15,8 @@ def test_host_layer_under_sanitizers_with_stubbed_launchers(tmp_path):
     r = subprocess.run([HIPCC, "--offload-arch=gfx950", "-O1", "-g", "-std=c++20",
                         "-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined", "-Xarch_host", "-fno-sanitize-recover=all",
                         "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument", "-o", exe,
-                        os.path.join(ROOT, "tests", "moe_sanitize_check.hip"), os.path.join(csrc, "moe_api.hip"), os.path.join(csrc, "adamw.hip")],
+                        os.path.join(ROOT, "tests", "moe_sanitize_check.hip"), os.path.join(csrc, "moe_api.hip"), os.path.join(csrc, "adamw.hip"),
+                        os.path.join(csrc, "tuning.hip")],
                        capture_output=True, text=True, timeout=600)
     assert r.returncode == 0, r.stderr[-3000:]
     # the HIP runtime keeps process-lifetime allocations: leak checking off, everything else on
