@@ -171,6 +171,7 @@ GROUPS = [
     ([700, 0, 1500, 3], 400, 48, 4112, 5),           # long groups with long rows of the gradient
     ([1, 1400], 100, 32, 8208, 0),
     ([690], 64, 16, 16400, 2),
+    ([1, 0, 3] * 170 + [5, 2], 100, 48, 80, 4),      # as many groups as there can be
 ]
 RECIPES = {"row": {}, "pow2": {"flags": 1}, "swapped": {"fmt_x": 1, "fmt_w": 1, "fmt_dy": 0}}
 

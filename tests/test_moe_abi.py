@@ -37,7 +37,7 @@ def test_route(lib, p):
         assert call(**{what: None}) == NULL, what
         assert call(**{what: p + 1}) == ALIGN, what
     assert call(logits=p + 2, flags=fp8.FP8_ROUTE_FP32) == ALIGN
-    for bad in ({"T": -1}, {"T": 1 << 31}, {"E": 0}, {"E": 513, "ld": 513}, {"k": 0}, {"k": 9}, {"E": 64, "ld": 64, "k": 17}, {"ld": 7}, {"T": 1 << 30, "k": 4}):
+    for bad in ({"T": -1}, {"T": 1 << 31}, {"T": 1 << 26}, {"E": 0}, {"E": 513, "ld": 513}, {"k": 0}, {"k": 9}, {"E": 64, "ld": 64, "k": 17}, {"ld": 7}, {"T": 1 << 30, "k": 4}):
         assert call(**bad) == SHAPE, bad
         assert fp8.fp8_last_error()
     assert call(flags=1) == ENUM
