@@ -206,7 +206,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void gemm_fp8_grouped_kerne
         constexpr int P = decltype(par_t)::value;
         using NS = std::integral_constant<int, P ^ 1>;
         // (operations younger than stage s + 1's loads: those of R - 2 stages, and now and then scale loads and stores, with which the
-        // wait is stricter than it need be)
+        // wait is stricter than it need be; a wait that counts the stores was timed and is no faster)
         wait_vmem_but_barrier<(R - 2) * NL>();
         const uint32_t ka = kofs(ca), ke = kofs(cb_e), ko = kofs(cb_o), to = (uint32_t)__builtin_amdgcn_readfirstlane((int)cur);
         const uint8_t* rs = smem + nxt;
@@ -388,10 +388,22 @@ hipError_t launch_gemm_fp8_grouped_rows(const GroupedGemm& g, hipStream_t st) {
     FP8K_FORMATS(launch_rows)
 }
 
+// Short groups here, where a tile of one or two steps has the next tile's operands and the last one's stores under way (whole backward
+// in us, the other file's 192 x 256 tiles of two steps at least / these of 128 x 256; at 256 rows its tiles of the rule below):
+//   rows a group        24        90        143       192        256
+//   64 of 1408 x 2048   321/303   361/331   380/345   400/366    412/404
+//   32 of 4096 x 1408   391/360   434/395   437/398   486/450    456/453
+//   128 of 768 x 2048   365/351   411/378   442/412   474/440    516/515
+//   16 of 2048 x 5632   336/332   345/343   366/362   392/388    402/409
+//   8 of 4096 x 4096    271/252   275/263   278/263   294/283    297/307
+//   8 of 4096 x 14336   887/871   975/954   996/980   1031/998   1007/1043
+//   8 of 14336 x 4096   862/803   888/831   912/850   965/887    903/924
+// The switch GEMM_STREAM: 0 always here, 2 and more never.
 template <int FA, int FB>
 static hipError_t launch_contract(const GroupedGemm& g, hipStream_t st) {
-    if (knob(KNOB_GEMM_STREAM) != 0) return launch_gemm_fp8_grouped_stream_contract(g, st);
-    return launch_t<FA, FB, 128, 256, 2, 2, 3, 8, true>(g, st);
+    const int stream = knob(KNOB_GEMM_STREAM);
+    if (stream == 0 || (stream < 0 && g.M <= 192 * g.E)) return launch_t<FA, FB, 128, 256, 2, 2, 3, 8, true>(g, st);
+    return launch_gemm_fp8_grouped_stream_contract(g, st);
 }
 hipError_t launch_gemm_fp8_grouped_contract(const GroupedGemm& g, hipStream_t st) { FP8K_FORMATS(launch_contract) }
 

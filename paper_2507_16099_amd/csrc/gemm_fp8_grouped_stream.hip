@@ -5,8 +5,8 @@
 // What is different: the tiles.  A workgroup first reads the offsets and leaves in LDS, behind the stages, where each group's rows
 // start and how many tiles the groups before it have; the tile list is then walked like that of one product.
 //   rows      a tile's rows end with its group; the rows behind the last group are tiles without codes, which come out as zeros
-//   contract  the length of the contraction is the group's.  A tile of up to 256 rows is one pair of K steps, which drains the tile
-//             before it in its first and itself from its second step on; so a tile's scales are requested a tile ahead.
+//   contract  the length of the contraction is the group's; a tile takes two pairs of K steps at least, with zeros past the group's
+//             rows (groups of up to 192 rows on average go to gemm_fp8_grouped.hip).  A tile's scales are requested a tile ahead.
 // (A lookup is a few LDS reads per tile, between two K steps.)
 // Tiles are dealt in rounds: the eight XCDs work on neighbouring runs of the tile order at any time, so that every round has tiles of
 // about the same group and all workgroups contract about the same length.  An XCD's own contiguous range of all tiles, as in the
@@ -21,7 +21,6 @@ namespace fp8k {
 
 namespace {
 
-enum { ST_ONLY = 4 };      // a pair that is a tile's first and last
 static_assert(st::LDS_BYTES + 12 * (GROUPED_MAX_EXPERTS + 2) <= 160 * 1024, "the groups' table");
 
 struct GroupedStreamArgs {
@@ -42,8 +41,7 @@ struct GroupedTile {
     int valid;
 };
 
-// SHORT: tiles of short groups take one pair of K steps (192-row tiles only: with it the 256-row ones spill fragments)
-template <int FA, int FB, int AF1, bool CONTRACT, bool SHORT = false>
+template <int FA, int FB, int AF1, bool CONTRACT>
 __global__ __launch_bounds__(st::NT) void gemm_fp8_grouped_stream_kernel(GroupedStreamArgs p) {
     using namespace st;
     static_assert(AF1 >= 2 && AF1 <= 4, "the A1 group has two to four fragments");
@@ -276,11 +274,10 @@ __global__ __launch_bounds__(st::NT) void gemm_fp8_grouped_stream_kernel(Grouped
         }(std::make_integer_sequence<int, 16>{});
     };
 
-    // pairs of K steps of a tile (an odd count of steps gets one of zeros): two at least, with SHORT one, except for a workgroup's
-    // first tile, in front of which there is nothing to drain
-    auto kpairs_of = [&](const GroupedTile& t, int j) {
-        const int pairs = ((t.k + BK - 1) / BK + 1) / 2, least = SHORT && j > 0 ? 1 : 2;
-        return pairs < least ? least : pairs;
+    // pairs of K steps of a tile (an odd count of steps gets one of zeros): a first and a last one at least
+    auto kpairs_of = [&](const GroupedTile& t) {
+        const int pairs = ((t.k + BK - 1) / BK + 1) / 2;
+        return pairs < 2 ? 2 : pairs;
     };
 
     // reciprocal scales of a tile, one row and one column per thread (correctly rounded divides).  The raw scales come into
@@ -315,12 +312,11 @@ __global__ __launch_bounds__(st::NT) void gemm_fp8_grouped_stream_kernel(Grouped
 
     // a pair of K steps (the B halves swap roles every step).  KIND: ST_FIRST(_DRAIN) = steps 0, 1 of a tile (step 0
     // starts the accumulators from zero; with _DRAIN the rest of the previous tile leaves in its phases 1-3; this tile's table of
-    // reciprocal scales is written in step 0), ST_MIDDLE, ST_LAST = the last two steps, ST_ONLY = both (the last steps also request the next tile's scales
+    // reciprocal scales is written in step 0), ST_MIDDLE, ST_LAST = the last two steps, which also request the next tile's scales
     // (refills fetch steps 0, 1 of tile `lt` = the next tile; the drain of this tile starts in phase 2 of the last step).
     auto pair = [&](auto kind_t, const GroupedTile& cur, const GroupedTile& lt, int k2_even, const Drain& dprev, const Drain& dcur, float* tab_cur, float* tab_nxt) {
         constexpr int KIND = decltype(kind_t)::value;
-        constexpr bool FIRST = KIND == ST_FIRST || KIND == ST_FIRST_DRAIN || KIND == ST_ONLY;
-        constexpr bool FD = KIND == ST_FIRST_DRAIN || KIND == ST_ONLY, LD = KIND == ST_LAST || KIND == ST_ONLY;
+        constexpr bool FIRST = KIND == ST_FIRST || KIND == ST_FIRST_DRAIN, FD = KIND == ST_FIRST_DRAIN, LD = KIND == ST_LAST;
         using Z = std::integral_constant<int, FIRST ? 1 : 0>;
         using NJ = StNoJobs;
         {
@@ -371,30 +367,19 @@ __global__ __launch_bounds__(st::NT) void gemm_fp8_grouped_stream_kernel(Grouped
     for (int j = 0; j < my_tiles; ++j) {
         float* tab_cur = tab0 + (j & 1) * (TAB / 4);
         float* tab_nxt = tab0 + (~j & 1) * (TAB / 4);
-        const int kpairs = kpairs_of(cur, j);
-        GroupedTile nxt;
-        bool done = false;
-        if constexpr (SHORT) {
-            if (kpairs == 1) {
-                nxt = tile_of(j + 1);
-                pair(std::integral_constant<int, ST_ONLY>{}, cur, nxt, 0, drain_of(prev, j - 1), drain_of(cur, j), tab_cur, tab_nxt);
-                done = true;
-            }
+        const int kpairs = kpairs_of(cur);
+        {
+            const Drain dprev = drain_of(prev, j - 1);
+            if (j == 0) pair(std::integral_constant<int, ST_FIRST>{}, cur, cur, 2 * BK, dprev, dprev, tab_cur, tab_nxt);
+            else pair(std::integral_constant<int, ST_FIRST_DRAIN>{}, cur, cur, 2 * BK, dprev, dprev, tab_cur, tab_nxt);
         }
-        if (!done) {
-            {
-                const Drain dprev = drain_of(prev, j - 1);
-                if (j == 0) pair(std::integral_constant<int, ST_FIRST>{}, cur, cur, 2 * BK, dprev, dprev, tab_cur, tab_nxt);
-                else pair(std::integral_constant<int, ST_FIRST_DRAIN>{}, cur, cur, 2 * BK, dprev, dprev, tab_cur, tab_nxt);
-            }
-            for (int kp = 1; kp < kpairs - 1; ++kp) {
-                const Drain none = drain_of(cur, j);
-                pair(std::integral_constant<int, ST_MIDDLE>{}, cur, cur, (2 * kp + 2) * BK, none, none, tab_cur, tab_nxt);
-            }
-            nxt = tile_of(j + 1);
-            const Drain dcur = drain_of(cur, j);
-            pair(std::integral_constant<int, ST_LAST>{}, cur, nxt, 0, dcur, dcur, tab_cur, tab_nxt);
+        for (int kp = 1; kp < kpairs - 1; ++kp) {
+            const Drain none = drain_of(cur, j);
+            pair(std::integral_constant<int, ST_MIDDLE>{}, cur, cur, (2 * kp + 2) * BK, none, none, tab_cur, tab_nxt);
         }
+        const GroupedTile nxt = tile_of(j + 1);
+        const Drain dcur = drain_of(cur, j);
+        pair(std::integral_constant<int, ST_LAST>{}, cur, nxt, 0, dcur, dcur, tab_cur, tab_nxt);
         prev = cur;
         cur = nxt;
     }
@@ -411,11 +396,11 @@ __global__ __launch_bounds__(st::NT) void gemm_fp8_grouped_stream_kernel(Grouped
     }
 }
 
-template <int FA, int FB, int AF1, bool CONTRACT, bool SHORT = false>
+template <int FA, int FB, int AF1, bool CONTRACT>
 hipError_t launch_t(const GroupedGemm& g, hipStream_t st) {
     using namespace st;
     constexpr int TM = 32 * (4 + AF1);
-    auto kern = gemm_fp8_grouped_stream_kernel<FA, FB, AF1, CONTRACT, SHORT>;
+    auto kern = gemm_fp8_grouped_stream_kernel<FA, FB, AF1, CONTRACT>;
     static DynamicLdsOnce attr;
     if (hipError_t e = attr.ensure(reinterpret_cast<const void*>(kern), 160 * 1024); e != hipSuccess) return e;
     int64_t cus = compute_units();
@@ -438,7 +423,6 @@ hipError_t launch_rows(const GroupedGemm& g, int height, hipStream_t st) {
 }
 template <int FA, int FB>
 hipError_t launch_contract(const GroupedGemm& g, hipStream_t st) {
-    if (g.M <= 192 * g.E) return launch_t<FA, FB, 2, true, true>(g, st);
     const int64_t rows = gemm_fp8_stream_tile_m(g.N * g.E, g.K);
     return rows == 256 ? launch_t<FA, FB, 4, true>(g, st) : rows == 224 ? launch_t<FA, FB, 3, true>(g, st) : launch_t<FA, FB, 2, true>(g, st);
 }
