@@ -70,24 +70,23 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void gemm_fp8_grouped_kerne
     const int tiles_n = p.tiles_n, per_group = p.tiles_m * tiles_n;
     const int row_tiles = CONTRACT ? p.tiles_m * p.E : __builtin_amdgcn_readfirstlane(tiles_to[p.E + 1]);
     const int units = row_tiles * tiles_n;
-    const int slots = (int)gridDim.x / NUM_XCD;
-    const int u_first = ((int)blockIdx.x % NUM_XCD) * slots + (int)blockIdx.x / NUM_XCD, u_step = NUM_XCD * slots;
-    if (u_first >= units) return;
+    const TileShare share(units);
+    if (share.mine == 0) return;
     const int cols_all = CONTRACT ? p.K : p.N;
     const int64_t lda = p.lda, ldb = p.ldb;
 
     // ---- the tile whose operands are requested next: its panels, contracted codes, the step's first code
     v4i_t rsrc_a, rsrc_b;
-    int k_tile = 0, k_next = 0, u_next = u_first, tab_next = 0;
+    int k_tile = 0, k_next = 0, j_next = 0, tab_next = 0;
     auto enter_tile = [&] {
         int row = 0, rows = 1, n0 = 0, brow = 0;
         uint64_t pa = reinterpret_cast<uint64_t>(p.A), pb = reinterpret_cast<uint64_t>(p.B);
-        const bool real = u_next < units;
+        const bool real = j_next < share.mine;
         k_tile = 0;
         k_next = 0;
         if (real) {
-            const int e_c = CONTRACT ? u_next / per_group : 0;
-            const int rest = u_next - e_c * per_group, in_group = GROUP_M * tiles_n, most_m = CONTRACT ? p.tiles_m : row_tiles;
+            const int u = share[j_next], e_c = CONTRACT ? u / per_group : 0;
+            const int rest = u - e_c * per_group, in_group = GROUP_M * tiles_n, most_m = CONTRACT ? p.tiles_m : row_tiles;
             const int first_m = rest / in_group * GROUP_M, in = rest % in_group;
             const int gsize = most_m - first_m < GROUP_M ? most_m - first_m : GROUP_M;
             const int tm = first_m + in % gsize;
@@ -128,7 +127,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void gemm_fp8_grouped_kerne
             }
         }
         if (tid == 0) places[tab_next] = make_int4(row, rows, n0, k_tile);
-        u_next += u_step;
+        ++j_next;
         tab_next = tab_next + 1 == NTAB ? 0 : tab_next + 1;
     };
     auto advance = [&] {      // to the next step of the sequence (a tile without codes has one, of zeros)
@@ -229,7 +228,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void gemm_fp8_grouped_kerne
     };
 
     // ---- a tile's end: reciprocals of its scales, the results, and on to the next one
-    int tab = 0, u = u_first, left = 0;      // left: steps of the present tile to go
+    int tab = 0, j = 0, left = 0;      // left: steps of the present tile to go
     auto steps_of = [&](int slot) {
         const int k = __builtin_amdgcn_readfirstlane(places[slot].w);
         return k > BK ? (k + BK - 1) / BK : 1;
@@ -283,7 +282,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void gemm_fp8_grouped_kerne
             }
         }
         clear();
-        u += u_step;
+        ++j;
         tab = tab + 1 == NTAB ? 0 : tab + 1;
         left = steps_of(tab);
     };
@@ -292,12 +291,12 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void gemm_fp8_grouped_kerne
         step(I0{});
         if (--left == 0) {
             finish();
-            if (u >= units) break;
+            if (j == share.mine) break;
         }
         step(I1{});
         if (--left == 0) {
             finish();
-            if (u >= units) break;
+            if (j == share.mine) break;
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // trailing (out-of-range) refills must land before the LDS is handed back

@@ -67,16 +67,14 @@ __global__ __launch_bounds__(st::NT) void gemm_fp8_grouped_stream_kernel(Grouped
     const int tiles_n = p.tiles_n, per_group = p.tiles_m * tiles_n;
     const int row_tiles = CONTRACT ? p.tiles_m * p.E : __builtin_amdgcn_readfirstlane(tiles_to[p.E + 1]);
     const int units = row_tiles * tiles_n;
-    const int slots = gridDim.x / NUM_XCD;
-    const int xcd = blockIdx.x % NUM_XCD, slot = blockIdx.x / NUM_XCD;
-    const int u_first = xcd * slots + slot, u_step = NUM_XCD * slots;
-    if (u_first >= units) return;
-    const int my_tiles = (units - u_first + u_step - 1) / u_step;
+    const TileShare share(units);
+    const int my_tiles = share.mine;
+    if (my_tiles == 0) return;
 
     auto tile_of = [&](int j) {
         GroupedTile t;
         t.valid = (j < my_tiles) ? 1 : 0;
-        const int logical = t.valid ? u_first + j * u_step : u_first;      // a missing tile aliases a valid one (its loads are forced out of range)
+        const int logical = share[t.valid ? j : 0];      // a missing tile aliases a valid one (its loads are forced out of range)
         const int e_c = CONTRACT ? logical / per_group : 0;
         const int rest = logical - e_c * per_group, in_group = GROUP_M * tiles_n, most_m = CONTRACT ? p.tiles_m : row_tiles;
         const int first_m = (rest / in_group) * GROUP_M;

@@ -100,6 +100,24 @@ __device__ __forceinline__ GroupTile find_group_tile(const int32_t* __restrict__
     return t;
 }
 
+// A persistent workgroup's share of `units` tiles: whole rounds, in which each of the eight XCDs takes a run of `slots` neighbouring ones,
+// and its part of the last round, which is spread over the XCDs too, for each has its own way to memory (four experts 4096 x 14336 with
+// 30, 2, 0 and 70 rows 67 us with the last round's tiles on the first XCDs, 45 so; 400 tokens, two of eight, 133 and 130; more rounds alike).
+struct TileShare {
+    int first, last, full, mine, step;
+    __device__ __forceinline__ TileShare(int units) {
+        const int slots = (int)gridDim.x / 8, xcd = (int)blockIdx.x % 8, slot = (int)blockIdx.x / 8;
+        step = 8 * slots;
+        full = units / step;
+        const int rest = units - full * step, per = (rest + 7) / 8, at = xcd * per + slot;
+        first = xcd * slots + slot;
+        last = full * step + at;
+        mine = full + (slot < per && at < rest ? 1 : 0);
+    }
+    // the j-th tile of it
+    __device__ __forceinline__ int operator[](int j) const { return j < full ? first + j * step : last; }
+};
+
 // the rows of one group, where it lies in the padded order, and how many tiles of `height` rows the groups before it have
 struct GroupSpan { int row0, rows, pad0, tile0; };
 __device__ __forceinline__ GroupSpan find_group(const int32_t* __restrict__ offsets, int E, int M, int group, int height) {
