@@ -528,6 +528,8 @@ int fp8_grouped_linear_fwd_prequantized(const void* x, int64_t T, const int32_t*
  * exp_avg_sq = sqrt(v) * scale_v with one power-of-two scale per block, [(n + 255) / 256]
  * each; a nonzero root is never rounded to zero.  To start, codes of zero with any
  * power-of-two scales.  This step's update uses the moments before that rounding.
+ * Gradients have to be finite: one that is not spoils its element for good, and with 8-bit
+ * moments those of its block.
  * One launch, however many tensors: it reads them from a table in device memory.
  * fp8_adamw_table writes that table (fp8_adamw_table_bytes bytes) into HOST memory, from an
  * array in host memory of count descriptors whose pointers are device pointers, 16-byte
